@@ -52,6 +52,7 @@ typedef int32_t afx_status;
 
 #define AFX_F16 0
 #define AFX_BF16 1
+#define AFX_F32 2 /* only where an entry point names it (rows of new tokens beside a paged cache) */
 
 #define AFX_MODE_TOPK 0      /* keep the k channels of largest |x|, ties to the lower index */
 #define AFX_MODE_THRESHOLD 1 /* keep channels with |x| > tau (strict); tau < 0 keeps all   */
@@ -664,6 +665,113 @@ afx_status afx_layer_step_q4(afx_model* model, int layer, afx_state* state, int 
 afx_status afx_mlp_block_noalloc(const void* w_gu, const void* w_down, int dtype, int hidden, int mlp,
                                  const void* x, int T, int mode, int k_gu, float tau_gu, int k_down,
                                  float tau_down, float* y, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Paged key-value cache: sequences of their own lengths over pages of a common pool (serving
+ * several requests at once, where the contiguous caches of afx_layer_desc hold every stream at one
+ * position).  afx_paged_append puts the keys and values of new tokens into the pages, with the norm
+ * of each head and the rotation of the position on the way; afx_paged_attn lets the new tokens'
+ * queries attend to the pages -- one to a few new tokens per sequence (decoding, checking drafts) or
+ * whole prompts and chunks of them; afx_layer_step_paged is a decoder layer over such a cache.
+ * (Serving interface of this library; the paper decodes one sequence.)
+ *
+ * Sequence b has seq_len[b] positions, the new tokens' included.  Its new tokens are the rows
+ * tok_start[b] .. tok_start[b+1]-1 of every token-major argument, at its last positions:
+ * position of row tok_start[b] + i = seq_len[b] - (tok_start[b+1] - tok_start[b]) + i.
+ * tok_start = NULL: one new token per sequence, row b.  Rows behind the last sequence (a padded
+ * batch) are neither read nor written.
+ * Element d of position p of sequence b, kv head g, lies at
+ *     page_table[b * table_stride + p / page_size] * page_stride + (p % page_size) * pos_stride + g * head_stride + d
+ * of k_pages and of v_pages (position-major and head-major pages, K and V in one buffer or in two).
+ * Lengths, starts and page ids are device data and checked there (dev_status): a length outside
+ * [0, table_stride * page_size] is clamped (AFX_ERR_CAPACITY), a start outside [start before, n_tokens]
+ * likewise (AFX_ERR_INVALID_ARG); of a sequence with more than max_new new tokens the rows behind the first max_new are
+ * left out (AFX_ERR_CAPACITY); a position whose page id is outside [0, n_pages), or that is negative
+ * (more new tokens than positions), is not written and not attended to (AFX_ERR_INVALID_ARG).
+ * Two tokens of a call must not share a cache row, nor two sequences a page that one of them writes.
+ * ------------------------------------------------------------------------------------------ */
+
+typedef struct {
+    int32_t dtype;       /* AFX_F16 / AFX_BF16: type of the cache                                */
+    int32_t n_kv_heads;
+    int32_t head_dim;    /* 64 or 128                                                            */
+    int32_t page_size;   /* positions per page, 1 .. 2^20, any number                            */
+    int32_t n_pages;     /* pages of the pool                                                    */
+    int32_t n_seqs;      /* sequences of the call, 0 .. 65535                                    */
+    int32_t n_tokens;    /* rows of the token-major arguments (an upper bound of tok_start)      */
+    int32_t max_new;     /* most new tokens of any sequence (HOST knowledge; >= 1)               */
+    int64_t page_stride; /* elements from page to page, position to position, kv head to kv head: */
+    int64_t pos_stride;  /* multiples of 8, >= head_dim                                          */
+    int64_t head_stride;
+    int64_t table_stride; /* entries of a page_table row (pages a sequence can have)             */
+    void* k_pages;       /* DEVICE, 16-byte aligned                                              */
+    void* v_pages;
+    const int32_t* page_table; /* DEVICE [n_seqs][table_stride]                                  */
+    const int32_t* seq_len;    /* DEVICE [n_seqs]                                                */
+    const int32_t* tok_start;  /* DEVICE [n_seqs + 1] or NULL                                    */
+} afx_paged_kv;
+
+#define AFX_ROPE_NONE 0
+#define AFX_ROPE_PAIRS 1  /* rotates dims (2i, 2i + 1)                     */
+#define AFX_ROPE_HALVES 2 /* rotates dims (i, i + rotary_dim / 2)          */
+
+typedef struct {
+    int32_t x_dtype;    /* AFX_F32, AFX_F16, AFX_BF16: type of q, k and v                        */
+    int32_t n_heads;    /* query heads; a multiple of n_kv_heads                                 */
+    float eps;          /* of the norms                                                          */
+    int32_t rope_style; /* AFX_ROPE_*                                                            */
+    int32_t rotary_dim; /* first dims of a head that are rotated: a multiple of 16, <= head_dim  */
+    int32_t rope_len;   /* positions of the tables                                               */
+    const float* g_q;   /* DEVICE [head_dim] fp32 gains of the heads' RMS norms, or NULL (no     */
+    const float* g_k;   /* norm); 16-byte aligned                                                */
+    const float* rope_cos; /* DEVICE [rope_len][rotary_dim / 2] fp32: cos and sin of position *  */
+    const float* rope_sin; /* frequency, 16-byte aligned                                         */
+} afx_head_prep;
+
+/*
+ * New tokens into the cache.  Per head of q and of k: u = x * rsqrt(mean(x^2) + eps) * gain (where a
+ * gain is given), then pairs (a, b) of the rotated dims become (a cos - b sin, a sin + b cos) of the token's
+ * position; q goes to q_out, k into its cache row, rounded once; v goes into its cache row as it is.  fp32
+ * arithmetic.  A token at a position >= rope_len is left out (AFX_ERR_CAPACITY in dev_status).
+ *
+ *   q, k, v   DEVICE, x_dtype, rows of n_heads * head_dim, n_kv_heads * head_dim (twice) values; ldq, ldk, ldv: values from
+ *             row to row (multiples of 8); 16-byte aligned.  q | k | v in one row as the q|k|v operator leaves it: three
+ *             pointers, the same stride.  q may be NULL (no queries; q_out too).
+ *   q_out     DEVICE [n_tokens][n_heads][head_dim], q_out_dtype (any of the three), 16-byte aligned.  It may be q itself
+ *             where types and strides agree (ldq = n_heads * head_dim).
+ *   dev_status DEVICE int32 or NULL.
+ * One kernel, bound by HBM (a few tokens: by its latency).
+ */
+afx_status afx_paged_append(const afx_paged_kv* kv, const afx_head_prep* prep, const void* q, int64_t ldq,
+                            const void* k, int64_t ldk, const void* v, int64_t ldv, void* q_out, int q_out_dtype,
+                            int32_t* dev_status, void* stream);
+
+/* Bytes of DEVICE workspace afx_paged_attn needs (256-byte aligned) for this descriptor's dtype-independent sizes (head_dim,
+ * n_kv_heads, n_seqs, max_new) and n_heads; 0 where it needs none or for a bad descriptor.  The workspace carries nothing from call to call;
+ * two calls that may overlap (streams, graphs) need one each. */
+size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads);
+
+/*
+ * Attention of the new tokens over the cache:
+ *
+ *     out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale * q[t][h] . k_j),   over the visible positions j
+ *
+ * of the token's sequence and kv head h / (n_heads / n_kv_heads).  With the token at position p, j is visible when
+ * j <= p and (window = 0, or j > p - window, or j < sinks): a sliding window and a few first positions that stay visible.
+ * A token that sees nothing gets zeros (lse: -inf).  What lies at positions that no token sees, or that only other tokens
+ * see, has no influence (NaN and infinities included).
+ *
+ *   q         DEVICE rows of n_heads * head_dim values, ldq values from row to row (a multiple of 8), 16-byte aligned; q_dtype = the
+ *             cache's type, or AFX_F32 where max_new <= AFX_MAX_T (AFX_ERR_UNSUPPORTED above).
+ *   scale     of the scores; 0 = 1 / sqrt(head_dim).
+ *   out       DEVICE [n_tokens][n_heads][head_dim], out_dtype AFX_F16 / AFX_BF16, 16-byte aligned.
+ *   lse       DEVICE fp32 [n_tokens][n_heads] or NULL: log(sum_j p_j), for joining with positions kept elsewhere.
+ *   workspace as afx_paged_attn_workspace_bytes says.
+ * The sums' order is fixed by the sizes and lengths (same inputs on the same device give the same bits).
+ */
+afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads, float scale,
+                          int window, int sinks, void* out, int out_dtype, float* lse, void* workspace,
+                          size_t workspace_bytes, int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

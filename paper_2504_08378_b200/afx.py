@@ -12,14 +12,15 @@ from ctypes import c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 from . import build as _build
 
-F16, BF16 = 0, 1
+F16, BF16, F32 = 0, 1, 2
 OP_QKV, OP_O, OP_GU, OP_DOWN = 0, 1, 2, 3
 XL_OFF, XL_BOOKKEEP, XL_REUSE = 0, 1, 2
 BUF_H, BUF_QKV, BUF_ATTN, BUF_HM, BUF_XNORM, BUF_IDX, BUF_MISS, BUF_STATS, BUF_HINTS = range(9)
 STEP_QKV, STEP_ATTN, STEP_O, STEP_GU, STEP_DOWN = range(5)
 MODE_TOPK, MODE_THRESHOLD = 0, 1
 MAX_T = 8
-DTYPES = {"f16": F16, "bf16": BF16}
+ROPE_NONE, ROPE_PAIRS, ROPE_HALVES = 0, 1, 2
+DTYPES = {"f16": F16, "bf16": BF16, "f32": F32}  # f32: only where an entry point names it
 
 STATUS_NAMES = {
     0: "AFX_OK", 1: "AFX_ERR_INVALID_ARG", 2: "AFX_ERR_ALIGNMENT", 3: "AFX_ERR_CAPACITY",
@@ -118,6 +119,22 @@ class Q4Layer(ctypes.Structure):
     _fields_ = [("wq", c_void_p * 4), ("ldq_bytes", c_int64 * 4)]
 
 
+class PagedKV(ctypes.Structure):
+    """afx_paged_kv"""
+    _fields_ = [("dtype", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32), ("page_size", c_int32),
+                ("n_pages", c_int32), ("n_seqs", c_int32), ("n_tokens", c_int32), ("max_new", c_int32),
+                ("page_stride", c_int64), ("pos_stride", c_int64), ("head_stride", c_int64), ("table_stride", c_int64),
+                ("k_pages", c_void_p), ("v_pages", c_void_p), ("page_table", c_void_p), ("seq_len", c_void_p),
+                ("tok_start", c_void_p)]
+
+
+class HeadPrep(ctypes.Structure):
+    """afx_head_prep"""
+    _fields_ = [("x_dtype", c_int32), ("n_heads", c_int32), ("eps", c_float), ("rope_style", c_int32),
+                ("rotary_dim", c_int32), ("rope_len", c_int32), ("g_q", c_void_p), ("g_k", c_void_p),
+                ("rope_cos", c_void_p), ("rope_sin", c_void_p)]
+
+
 class AfxError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
@@ -188,6 +205,12 @@ def lib() -> ctypes.CDLL:
         L.afx_layer_step_q4.argtypes = [c_void_p, c_int, c_void_p, c_int, ctypes.POINTER(Q4Layer), c_void_p, c_void_p]
         L.afx_mlp_block_noalloc.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_int, c_int,
                                             c_float, c_int, c_float, c_void_p, c_void_p]
+        L.afx_paged_append.argtypes = [ctypes.POINTER(PagedKV), ctypes.POINTER(HeadPrep), c_void_p, c_int64, c_void_p, c_int64,
+                                       c_void_p, c_int64, c_void_p, c_int, c_void_p, c_void_p]
+        L.afx_paged_attn_workspace_bytes.restype = c_size_t
+        L.afx_paged_attn_workspace_bytes.argtypes = [ctypes.POINTER(PagedKV), c_int]
+        L.afx_paged_attn.argtypes = [ctypes.POINTER(PagedKV), c_void_p, c_int, c_int64, c_int, c_float, c_int, c_int,
+                                     c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
         _lib = L
     return _lib
 
@@ -457,3 +480,22 @@ def afx_layer_step_q4(model: int, layer: int, state: int, pos: int, q4: Q4Layer,
 def afx_layer_step_hosted(model: int, layer: int, state: int, pos: int, ops: HostedOps, stream=None, dev_status=None):
     _check("afx_layer_step_hosted", lib().afx_layer_step_hosted(model, int(layer), state, int(pos), ctypes.byref(ops),
                                                                 _ptr(dev_status), _stream(stream)))
+
+
+def afx_paged_append(kv: PagedKV, prep: HeadPrep, q, ldq: int, k, ldk: int, v, ldv: int, q_out, q_out_dtype, stream=None,
+                     dev_status=None):
+    _check("afx_paged_append",
+           lib().afx_paged_append(ctypes.byref(kv), ctypes.byref(prep), _ptr(q), int(ldq), _ptr(k), int(ldk), _ptr(v), int(ldv),
+                                  _ptr(q_out), _dt(q_out_dtype), _ptr(dev_status), _stream(stream)))
+
+
+def afx_paged_attn_workspace_bytes(kv: PagedKV, n_heads: int) -> int:
+    return int(lib().afx_paged_attn_workspace_bytes(ctypes.byref(kv), int(n_heads)))
+
+
+def afx_paged_attn(kv: PagedKV, q, q_dtype, ldq: int, n_heads: int, scale: float, window: int, sinks: int, out, out_dtype,
+                   lse=None, workspace=None, workspace_bytes: int = 0, stream=None, dev_status=None):
+    _check("afx_paged_attn",
+           lib().afx_paged_attn(ctypes.byref(kv), _ptr(q), _dt(q_dtype), int(ldq), int(n_heads), float(scale), int(window),
+                                int(sinks), _ptr(out), _dt(out_dtype), _ptr(lse), _ptr(workspace), int(workspace_bytes),
+                                _ptr(dev_status), _stream(stream)))

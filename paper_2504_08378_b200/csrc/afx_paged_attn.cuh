@@ -1,0 +1,80 @@
+// Attention over the paged cache: arguments, and one token row on the fp32 pipe.
+#pragma once
+
+#include "afx_attn.cuh"
+#include "afx_paged.cuh"
+
+namespace afx {
+
+struct PagedAttnArgs {
+    PagedView w;
+    PagedMask mask;
+    const char* q;   // q_type rows of heads * D values
+    int64_t ldq;     // in values
+    int q_type;
+    int heads, rep;  // rep = heads / n_kv
+    float scale;     // of the scores, times log2(e)
+    uint16_t* out;
+    int out_type;
+    float* lse;      // or NULL
+};
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <int CT>
+__device__ __forceinline__ float2 pair_values(uint32_t r) {
+    if constexpr (CT == AFX_F16) return __half22float2(*reinterpret_cast<const __half2*>(&r));
+    return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u));
+}
+
+__device__ __forceinline__ float typed_value(const char* p, int type, int64_t i) {
+    if (type == AFX_F32) return reinterpret_cast<const float*>(p)[i];
+    const uint16_t b = reinterpret_cast<const uint16_t*>(p)[i];
+    return type == AFX_F16 ? bits_to_float<AFX_F16>(b) : bits_to_float<AFX_BF16>(b);
+}
+__device__ __forceinline__ uint16_t typed_bits(float v, int type) {
+    return type == AFX_F16 ? float_to_bits<AFX_F16>(v) : float_to_bits<AFX_BF16>(v);
+}
+
+// Running softmax of one row in a warp: a lane owns D / 32 neighbouring dims.
+template <int D>
+struct RowState {
+    float m = -INFINITY, l = 0.0f, acc[D / 32];
+};
+
+// Positions [from, to) of (sequence b, kv head g) added to the row with query q (times scale * log2 e).
+template <int D, int CT>
+__device__ __forceinline__ void attend_row(const PagedView& w, int b, int g, const float (&q)[D / 32], int from, int to,
+                                           RowState<D>& s) {
+    constexpr int E = D / 32;
+    const int lane = lane_id();
+    for (int p = from; p < to; ++p) {
+        const int64_t at = paged_row(w, b, p, g);
+        if (at < 0) {
+            if (lane == 0) report_status(w.status, AFX_ERR_INVALID_ARG);
+            continue;
+        }
+        const uint32_t* kr = reinterpret_cast<const uint32_t*>(w.k + at) + lane * (E / 2);
+        const uint32_t* vr = reinterpret_cast<const uint32_t*>(w.v + at) + lane * (E / 2);
+        float d = 0.0f;
+        float v[E];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 kk = pair_values<CT>(kr[i]), vv = pair_values<CT>(vr[i]);
+            d = fmaf(q[2 * i], kk.x, d);
+            d = fmaf(q[2 * i + 1], kk.y, d);
+            v[2 * i] = vv.x;
+            v[2 * i + 1] = vv.y;
+        }
+        d = warp_sum(d);
+        const float mn = fmaxf(s.m, d);
+        const float ref = mn == -INFINITY ? 0.0f : mn;
+        const float f = fast_exp2(s.m - ref), pw = fast_exp2(d - ref);
+        s.m = mn;
+        s.l = fmaf(s.l, f, pw);
+#pragma unroll
+        for (int i = 0; i < E; ++i) s.acc[i] = fmaf(s.acc[i], f, pw * v[i]);
+    }
+}
+
+}  // namespace afx
