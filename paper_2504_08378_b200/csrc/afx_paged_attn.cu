@@ -1,5 +1,5 @@
 // afx_paged_attn: checks and the choice of the kernel.
-#include "afx_paged_attn.cuh"
+#include "afx_paged_few.cuh"
 
 namespace afx {
 
@@ -65,7 +65,9 @@ static afx_status attn_args(const afx_paged_kv* kv, int n_heads, int32_t* dev_st
 extern "C" size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads) {
     afx::PagedAttnArgs a = {};
     if (afx::attn_args(kv, n_heads, nullptr, &a) != AFX_OK) return 0;
-    return 0;
+    if (kv->max_new > AFX_MAX_T) return 0;
+    const size_t bytes = static_cast<size_t>(2) * afx::kFewMaxBlocks * afx::few_slot_floats(kv->head_dim) * sizeof(float);
+    return (bytes + 255) / 256 * 256;
 }
 
 extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads,
@@ -98,6 +100,12 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
     a.out_type = out_dtype;
     a.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (kv->max_new <= AFX_MAX_T) {
+        PagedFewArgs f = {};
+        f.a = a;
+        f.slots = static_cast<float*>(workspace);
+        return launch_paged_few(kv->dtype, D, f, st);
+    }
     if (D == 128)
         return kv->dtype == AFX_F16 ? launch_rows<128, AFX_F16>(a, st) : launch_rows<128, AFX_BF16>(a, st);
     return kv->dtype == AFX_F16 ? launch_rows<64, AFX_F16>(a, st) : launch_rows<64, AFX_BF16>(a, st);

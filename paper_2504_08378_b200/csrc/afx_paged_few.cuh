@@ -1,0 +1,641 @@
+// Attention of few new tokens per sequence over the paged cache: the cached positions of all sequences are one list of
+// tiles, cut into equal ranges, one per block; what a range leaves unfinished is joined by a second kernel.
+//
+// An item is (sequence, kv head, group of up to 16 rows); its rows are the sequence's new tokens times the query heads of
+// the kv head.  Its positions are those that any of its tokens sees: the first `few` ones and the window from `low` on,
+// counted through without the gap between them.  A tile is 64 of them; a block walks its range of the list, the
+// positions of a tile 16 to a warp (a chunk), every warp with a ring of chunks of its own that cp.async fills across the borders of
+// items: nobody waits for another warp before an item's end.  A chunk is two matrix products on the tensor cores
+// (16 rows x 16 positions x D and 16 rows x D x 16 positions); softmax is online and in base 2, the weights are split
+// into two 16-bit halves so that none of their bits are lost, fp32 queries likewise.  Where there are at most 8 rows (one new token
+// and up to 8 heads per kv head), the two halves are the 16 rows of a product.
+//
+// Bound by HBM: 16 positions are 8 KB of K and V at D = 128 and about 250 instructions of a warp, an SM's share of the
+// bandwidth is 8 KB every 190 ns = 1400 issue slots.  Two blocks of 4 warps per SM with rings of 96 KB each keep
+// up to 128 KB of an SM on their way.
+#pragma once
+
+#include "afx_attn_mma.cuh"
+#include "afx_paged_attn.cuh"
+
+namespace afx {
+
+constexpr int kFewWarps = 4;
+constexpr int kFewThreads = kFewWarps * 32;
+constexpr int kFewChunk = 16;
+constexpr int kFewTile = kFewChunk * kFewWarps;
+constexpr int kFewMaxBlocks = 296;  // ranges at most (two blocks on each of 148 SMs); sizes the workspace
+constexpr int kFewRows = 16;
+
+template <int D>
+struct FewCfg {
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kChunkBytes = 2 * kFewChunk * D * 2;  // K rows, V rows
+    static constexpr int kRing = kFewWarps * kStages * kChunkBytes;
+    static constexpr int kMerge = kFewWarps * 1024 * 4;        // [warp][1024 values of the partial outputs]
+    static constexpr int kDyn = kRing + kMerge;
+};
+
+// An unfinished item's sums in the workspace: slot 2 i is the first piece of range i, 2 i + 1 a later one.
+__host__ __device__ constexpr int few_slot_floats(int D) { return kFewRows * (D + 2); }  // m[16], l[16], acc[16][D]
+
+struct PagedFewArgs {
+    PagedAttnArgs a;
+    int rows_per_group;  // 8 (packed) or 16
+    float* slots;
+};
+
+afx_status launch_paged_few(int dtype, int D, PagedFewArgs& f, cudaStream_t st);  // afx_paged_few.cu
+inline bool few_packed(int max_new, int rep) { return static_cast<int64_t>(max_new) * rep <= 8; }
+
+// A sequence in the list of tiles.
+struct FewSeq {
+    SeqSpan s;
+    int few, low, nv;  // visible positions: [0, few) and low ..; nv of them
+    int tiles;         // per item
+    int items;         // kv heads times row groups
+};
+
+__device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool report) {
+    FewSeq q;
+    q.s = paged_span(f.a.w, b, report);
+    const int first = max(q.s.first, 0), end = min(q.s.len, q.s.first + q.s.n);
+    q.low = paged_low(f.a.mask, first);
+    q.few = paged_few(f.a.mask, q.low);
+    q.nv = max(end - q.low, 0) + (end > q.low ? q.few : 0);
+    q.items = q.s.n > 0 ? f.a.w.n_kv * ((q.s.n * f.a.rep + f.rows_per_group - 1) / f.rows_per_group) : 0;
+    q.tiles = (q.nv + kFewTile - 1) / kFewTile;
+    return q;
+}
+
+// The list's length; scratch[i] = tiles in front of the sequences of thread i (kFewThreads + kFewWarps values).  All threads call it.
+__device__ __forceinline__ int64_t few_list_total(const PagedFewArgs& f, int64_t* scratch, bool report) {
+    const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads, tid = threadIdx.x;
+    int64_t mine = 0;
+    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
+        const FewSeq q = few_seq(f, i, report);
+        mine += static_cast<int64_t>(q.tiles) * q.items;
+    }
+    // inclusive sums over the threads
+    int64_t incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane_id() >= o) incl += up;
+    }
+    if (lane_id() == 31) scratch[kFewThreads + warp_id()] = incl;
+    __syncthreads();
+    int64_t base = 0;
+    for (int w = 0; w < warp_id(); ++w) base += scratch[kFewThreads + w];
+    scratch[tid] = base + incl - mine;  // tiles in front of this thread's sequences
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < kFewWarps; ++w) total += scratch[kFewThreads + w];
+    return total;
+}
+// The sequence that holds tile `at` (0 <= at < total) and the tiles in front of it; one thread's work, from scratch.
+__device__ __forceinline__ int few_find(const PagedFewArgs& f, const int64_t* scratch, int64_t at, int64_t& before) {
+    const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads;
+    int lo = 0, hi = kFewThreads - 1;
+    while (lo < hi) {  // the last thread whose sequences start at or before the tile
+        const int mid = (lo + hi + 1) >> 1;
+        if (scratch[mid] <= at) lo = mid; else hi = mid - 1;
+    }
+    int64_t sum = scratch[lo];
+    int b = lo * per;
+    for (; b < min(n, (lo + 1) * per) - 1; ++b) {
+        const FewSeq q = few_seq(f, b, false);
+        const int64_t t = static_cast<int64_t>(q.tiles) * q.items;
+        if (sum + t > at) break;
+        sum += t;
+    }
+    before = sum;
+    return b;
+}
+__device__ __forceinline__ int64_t few_range(int64_t total, int i, int blocks) { return total * i / blocks; }
+
+// A block's walk over its range: the pieces of items in it, one after the other.
+struct FewWalk {
+    FewSeq q;
+    int b, item;
+    int t0, t1;         // this piece's tiles of the item
+    int64_t left;       // tiles of the range behind this piece
+    bool more;          // there is a piece
+
+    __device__ __forceinline__ void cut() {
+        t1 = static_cast<int>(min(static_cast<int64_t>(q.tiles), t0 + left));
+        left -= t1 - t0;
+    }
+    __device__ __forceinline__ void next(const PagedFewArgs& f) {
+        if (left <= 0) {
+            more = false;
+            return;
+        }
+        t0 = 0;
+        if (++item == q.items) {
+            item = 0;
+            do {
+                if (++b >= f.a.w.n_seqs) {  // (lengths that changed under the call)
+                    more = false;
+                    return;
+                }
+                q = few_seq(f, b, false);
+            } while (q.tiles == 0 || q.items == 0);
+        }
+        cut();
+    }
+    // chunks of this piece that warp w takes: w, w + warps, ..
+    __device__ __forceinline__ int chunks(int w) const {
+        const int n = (min(q.nv, t1 * kFewTile) - t0 * kFewTile + kFewChunk - 1) / kFewChunk;
+        return n > w ? (n - w + kFewWarps - 1) / kFewWarps : 0;
+    }
+};
+
+__device__ __forceinline__ void few_copy16(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(at));
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(at));
+}
+template <int CT>
+__device__ __forceinline__ void few_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (CT == AFX_F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// (a, b) rounded to the cache's type, and what that left out
+template <int CT>
+__device__ __forceinline__ void few_split(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack2_bits<CT>(a, b);
+    const float2 f = pair_values<CT>(hi);
+    lo = pack2_bits<CT>(a - f.x, b - f.y);
+}
+
+// Row r (0 .. 15) of row group g of a piece: token row and position, query head.  live: it exists.
+struct FewRow {
+    int t, pos, h;
+    bool live;
+};
+__device__ __forceinline__ FewRow few_row(const PagedFewArgs& f, const FewSeq& q, int kv_head, int group, int r) {
+    const int rr = group * f.rows_per_group + r, i = rr / f.a.rep;
+    FewRow o;
+    o.live = r < f.rows_per_group && i < q.s.n;
+    o.t = q.s.row0 + i;
+    o.pos = q.s.first + i;
+    o.h = kv_head * f.a.rep + rr - i * f.a.rep;
+    return o;
+}
+__device__ __forceinline__ int few_pos(const FewSeq& q, int v) { return v < q.few ? v : v - q.few + q.low; }
+__device__ __forceinline__ bool few_sees(const PagedMask& m, int pos, int p) {
+    return p <= pos && (m.window == 0 || p > pos - m.window || p < m.sinks);
+}
+
+template <int D, int CT, bool PACK, bool QF32>
+__global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs f) {
+    using Cfg = FewCfg<D>;
+    constexpr int ST = Cfg::kStages, NK = D / 16, NT = D / 8, PIECES = D / 8;
+    constexpr int NR = PACK ? 1 : 2;                       // rows of a lane: gid (and gid + 8)
+    constexpr float kUp = CT == AFX_F16 ? 1024.0f : 1.0f;  // weights are carried times this: the low halves of small ones stay normal
+    extern __shared__ __align__(128) unsigned char dyn[];
+    __shared__ uint32_t stage_mask[kFewWarps][ST];
+    __shared__ float sm_m[kFewWarps][kFewRows], sm_l[kFewWarps][kFewRows];
+    __shared__ int64_t start_before;
+    __shared__ int start_b;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int gid = lane >> 2, tig = lane & 3;
+    float* merge = reinterpret_cast<float*>(dyn + Cfg::kRing);
+    int64_t* scratch = reinterpret_cast<int64_t*>(merge);  // (before the first merge)
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dyn)) + warp * ST * Cfg::kChunkBytes;
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    const int64_t total = few_list_total(f, scratch, blockIdx.x == 0);
+    const int64_t lo = few_range(total, blockIdx.x, gridDim.x), hi = few_range(total, blockIdx.x + 1, gridDim.x);
+    if (lo >= hi) return;
+    if (tid == 0) {
+        int64_t before;
+        start_b = few_find(f, scratch, lo, before);
+        start_before = before;
+    }
+    __syncthreads();
+    FewWalk con;
+    con.b = start_b;
+    con.q = few_seq(f, con.b, false);
+    con.item = static_cast<int>((lo - start_before) / con.q.tiles);
+    con.t0 = static_cast<int>((lo - start_before) - static_cast<int64_t>(con.item) * con.q.tiles);
+    con.left = hi - lo;
+    con.more = true;
+    con.cut();
+
+    // ---- the ring's filling side: chunk after chunk of this warp, across pieces
+    FewWalk pro = con;
+    int pk = 0, pn = pro.chunks(warp), p_stage = 0;
+    int64_t p_off = -1;  // lane j < 16: offset of the next chunk's position j; -1: leave out
+    auto look_up = [&]() {
+        while (pro.more && pk >= pn) {
+            pro.next(f);
+            pk = 0;
+            pn = pro.more ? pro.chunks(warp) : 0;
+        }
+        if (!pro.more) return;
+        const int v = pro.t0 * kFewTile + (pk * kFewWarps + warp) * kFewChunk + (lane & 15);
+        p_off = -1;
+        if (v < pro.q.nv) {
+            const int groups = pro.q.items / f.a.w.n_kv;
+            p_off = paged_row(f.a.w, pro.b, few_pos(pro.q, v), pro.item / groups);
+            if (p_off < 0) report_status(f.a.w.status, AFX_ERR_INVALID_ARG);
+        }
+    };
+    auto issue = [&]() {
+        if (pro.more) {
+            const uint32_t at = ring + p_stage * Cfg::kChunkBytes;
+            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, p_off >= 0) & 0xFFFFu;
+            if (lane == 0) stage_mask[warp][p_stage] = mask;
+            constexpr int RPI = 32 / PIECES;  // rows per instruction
+#pragma unroll
+            for (int i = 0; i < kFewChunk / RPI; ++i) {
+                const int row = i * RPI + lane / PIECES, piece = lane % PIECES;
+                const int64_t off = __shfl_sync(0xFFFFFFFFu, p_off, row);
+                const int64_t e = (off < 0 ? 0 : off) + piece * 8;
+                const uint32_t d = at + row * (D * 2) + ((piece ^ (row & 7)) << 4);
+                few_copy16(d, f.a.w.k + e, off < 0 ? 0 : 16);
+                few_copy16(d + kFewChunk * D * 2, f.a.w.v + e, off < 0 ? 0 : 16);
+            }
+            p_stage = p_stage + 1 == ST ? 0 : p_stage + 1;
+            ++pk;
+            look_up();
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    look_up();
+#pragma unroll
+    for (int i = 0; i < ST - 1; ++i) issue();
+
+    int stage = 0;
+    bool first_piece = true;
+    for (; con.more; con.next(f), first_piece = false) {
+        const FewSeq& q = con.q;
+        const int groups = q.items / f.a.w.n_kv, kv_head = con.item / groups, group = con.item - kv_head * groups;
+        // ---- queries of the lane's rows as fragments of the first product
+        uint32_t qa[NK][4], ql[QF32 && !PACK ? NK : 1][4];
+        float unit[NR];
+        int pos[NR];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const FewRow r = few_row(f, q, kv_head, group, gid + 8 * e);
+            if (e < NR) {
+                unit[e < NR ? e : 0] = f.a.scale;
+                pos[e < NR ? e : 0] = r.live ? r.pos : -1;
+            }
+            const bool row = r.live && e < NR;
+            const int64_t at = row ? r.t * f.a.ldq + static_cast<int64_t>(r.h) * D : 0;
+            if constexpr (QF32) {
+                const float* src = reinterpret_cast<const float*>(f.a.q) + at;
+                float2 x[2 * NK];
+                float big = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 2 * NK; ++i) {
+                    x[i] = row ? *reinterpret_cast<const float2*>(src + 8 * i + 2 * tig) : make_float2(0.0f, 0.0f);
+                    big = fmaxf(big, fmaxf(fabsf(x[i].x), fabsf(x[i].y)));
+                }
+                float up = 1.0f;
+                if constexpr (CT == AFX_F16) {  // the row's largest value lands in [2^9, 2^10): fp16's range holds both halves
+                    big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
+                    big = fmaxf(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
+                    const int ex = min(max(static_cast<int>((__float_as_uint(big) >> 23) & 0xFFu) - 127, -100), 110);
+                    up = __uint_as_float(static_cast<uint32_t>(127 + 9 - ex) << 23);
+                    if (e < NR) unit[e < NR ? e : 0] = f.a.scale * __uint_as_float(static_cast<uint32_t>(127 - 9 + ex) << 23);
+                }
+                if (e < NR) {
+#pragma unroll
+                    for (int i = 0; i < 2 * NK; ++i) {
+                        uint32_t h16, l16;
+                        few_split<CT>(x[i].x * up, x[i].y * up, h16, l16);
+                        qa[i >> 1][2 * (i & 1) + e] = h16;
+                        if constexpr (PACK) qa[i >> 1][2 * (i & 1) + 1] = l16;
+                        else ql[i >> 1][2 * (i & 1) + e] = l16;
+                    }
+                }
+            } else {
+                const uint16_t* src = reinterpret_cast<const uint16_t*>(f.a.q) + at;
+#pragma unroll
+                for (int i = 0; i < 2 * NK; ++i)
+                    qa[i >> 1][2 * (i & 1) + e] = row ? *reinterpret_cast<const uint32_t*>(src + 8 * i + 2 * tig) : 0u;
+            }
+        }
+        float m[NR], l[NR], o[NT][4];
+#pragma unroll
+        for (int e = 0; e < NR; ++e) {
+            m[e] = -INFINITY;
+            l[e] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[i][x] = 0.0f;
+        const int last = q.s.first + q.s.n - 1;
+        const int n_chunks = con.chunks(warp);
+        for (int k = 0; k < n_chunks; ++k) {
+            const int v0 = con.t0 * kFewTile + (k * kFewWarps + warp) * kFewChunk;
+            asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
+            __syncwarp();
+            const uint32_t kat = ring + stage * Cfg::kChunkBytes, vat = kat + kFewChunk * D * 2;
+            const uint32_t vm = stage_mask[warp][stage];
+            float c[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            float cl[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            {
+                const int row = (lane & 7) + ((lane & 16) >> 1), half = (lane >> 3) & 1;
+#pragma unroll
+                for (int j = 0; j < NK; ++j) {
+                    uint32_t kb[4];
+                    ldmatrix_x4(kb, kat + row * (D * 2) + (((2 * j + half) ^ (row & 7)) << 4));
+                    few_mma<CT>(c[0], qa[j], kb[0], kb[1]);
+                    few_mma<CT>(c[1], qa[j], kb[2], kb[3]);
+                    if constexpr (QF32 && !PACK) {
+                        few_mma<CT>(cl[0], ql[j], kb[0], kb[1]);
+                        few_mma<CT>(cl[1], ql[j], kb[2], kb[3]);
+                    }
+                }
+            }
+            float s[NR][4];  // positions 2 tig, 2 tig + 1, 8 + 2 tig, 9 + 2 tig
+#pragma unroll
+            for (int e = 0; e < NR; ++e)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float hi32 = c[x >> 1][2 * e + (x & 1)];
+                    float t = hi32;
+                    if constexpr (PACK) { if constexpr (QF32) t = whole(hi32, c[x >> 1][2 + (x & 1)]); }
+                    else if constexpr (QF32) t = whole(hi32, cl[x >> 1][2 * e + (x & 1)]);
+                    s[e][x] = t * unit[e];
+                }
+            // every row sees the whole chunk, in the usual case
+            bool all = vm == 0xFFFFu;
+            if (q.s.n > 1 && all) {
+                const int p0 = few_pos(q, v0), p1 = few_pos(q, v0 + kFewChunk - 1);
+                all = p1 <= q.s.first && (f.a.mask.window == 0 || p0 > last - f.a.mask.window || p1 < f.a.mask.sinks);
+            }
+            if (!all) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int j = 8 * (x >> 1) + 2 * tig + (x & 1), p = few_pos(q, v0 + j);
+#pragma unroll
+                    for (int e = 0; e < NR; ++e)
+                        if (!((vm >> j) & 1u) || !few_sees(f.a.mask, pos[e], p)) s[e][x] = -INFINITY;
+                }
+            }
+            uint32_t pa[4], pl[4];
+            float grow[NR], ref[NR];
+            bool moved = false;
+#pragma unroll
+            for (int e = 0; e < NR; ++e) {
+                float mn = fmaxf(fmaxf(s[e][0], s[e][1]), fmaxf(s[e][2], s[e][3]));
+                mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 1));
+                mn = fmaxf(mn, __shfl_xor_sync(0xFFFFFFFFu, mn, 2));
+                mn = fmaxf(mn, m[e]);
+                ref[e] = mn == -INFINITY ? 0.0f : mn;
+                grow[e] = fast_exp2(m[e] - ref[e]);  // 0 where nothing was seen before
+                moved |= mn > m[e];
+                m[e] = mn;
+            }
+            if (__any_sync(0xFFFFFFFFu, moved)) {
+#pragma unroll
+                for (int e = 0; e < NR; ++e) l[e] *= grow[e];
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) o[i][x] *= grow[PACK ? 0 : x >> 1];
+            }
+#pragma unroll
+            for (int e = 0; e < NR; ++e) {
+                float p[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) p[x] = fast_exp2(s[e][x] - ref[e]) * kUp;
+                l[e] += (p[0] + p[1]) + (p[2] + p[3]);
+                if constexpr (PACK) {
+                    few_split<CT>(p[0], p[1], pa[0], pa[1]);
+                    few_split<CT>(p[2], p[3], pa[2], pa[3]);
+                } else {
+                    few_split<CT>(p[0], p[1], pa[e], pl[e]);
+                    few_split<CT>(p[2], p[3], pa[2 + e], pl[2 + e]);
+                }
+            }
+            {
+                const int row = (lane & 7) + (lane & 8), half = lane >> 4;
+#pragma unroll
+                for (int i = 0; i < NT; i += 2) {
+                    uint32_t vb[4];
+                    ldmatrix_x4_trans(vb, vat + row * (D * 2) + (((i + half) ^ (row & 7)) << 4));
+                    few_mma<CT>(o[i], pa, vb[0], vb[1]);
+                    few_mma<CT>(o[i + 1], pa, vb[2], vb[3]);
+                    if constexpr (!PACK) {
+                        few_mma<CT>(o[i], pl, vb[0], vb[1]);
+                        few_mma<CT>(o[i + 1], pl, vb[2], vb[3]);
+                    }
+                }
+            }
+            __syncwarp();
+            stage = stage + 1 == ST ? 0 : stage + 1;
+            issue();
+        }
+
+        // ---- the warps' sums meet
+        uint32_t bad = 0;  // rows whose sums are not finite: a value that the row does not see may have been NaN or infinite
+#pragma unroll
+        for (int e = 0; e < NR; ++e) {
+            l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 1);
+            l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 2);
+            bool fin = true;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    float& t = o[i][2 * e + x];
+                    if constexpr (PACK) t = whole(t, o[i][2 + x]);
+                    t *= 1.0f / kUp;
+                    fin &= fabsf(t) <= 3.402823466e38f;
+                }
+            const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, !fin);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if ((lanes >> (4 * r)) & 0xFu) bad |= 1u << (r + 8 * e);
+        }
+        if (tig == 0) {
+#pragma unroll
+            for (int e = 0; e < NR; ++e) {
+                sm_m[warp][gid + 8 * e] = m[e];
+                sm_l[warp][gid + 8 * e] = l[e] * (1.0f / kUp);
+            }
+        }
+        const bool whole_item = con.t0 == 0 && con.t1 == q.tiles;
+        float* slot = f.slots + static_cast<int64_t>(2 * blockIdx.x + (first_piece ? 0 : 1)) * few_slot_floats(D);
+        // 1024 values of a warp at a time: 8 rows x 128 dims, 16 rows x 64 dims (twice), 8 rows x 64 dims
+        constexpr int RW = PACK ? 8 : 16, DW = PACK ? D : 64;
+#pragma unroll
+        for (int part = 0; part < D / DW; ++part) {
+            float* mine = merge + warp * 1024;
+#pragma unroll
+            for (int i = 0; i < DW / 8; ++i)
+#pragma unroll
+                for (int e = 0; e < NR; ++e) {
+                    const float* t = &o[part * (DW / 8) + i][2 * e];
+                    *reinterpret_cast<float2*>(mine + (gid + 8 * e) * DW + 8 * i + 2 * tig) = make_float2(t[0], t[1]);
+                }
+            __syncwarp();
+            for (uint32_t left = bad; left != 0; left &= left - 1) {  // again, over what the row sees alone
+                const int r = __ffs(left) - 1;
+                const FewRow fr = few_row(f, q, kv_head, group, r);
+                RowState<D> st;
+                float qv[D / 32];
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {
+                    st.acc[x] = 0.0f;
+                    qv[x] = fr.live ? f.a.scale * typed_value(f.a.q, f.a.q_type, fr.t * f.a.ldq + static_cast<int64_t>(fr.h) * D + lane * (D / 32) + x) : 0.0f;
+                }
+                for (int k = 0; fr.live && k < n_chunks; ++k) {
+                    const int v0 = con.t0 * kFewTile + (k * kFewWarps + warp) * kFewChunk;
+                    for (int v = v0; v < min(v0 + kFewChunk, q.nv); ++v) {
+                        const int p = few_pos(q, v);
+                        if (few_sees(f.a.mask, fr.pos, p)) attend_row<D, CT>(f.a.w, con.b, kv_head, qv, p, p + 1, st);
+                    }
+                }
+#pragma unroll
+                for (int x = 0; x < D / 32; ++x) {
+                    const int d = lane * (D / 32) + x - part * DW;
+                    if (d >= 0 && d < DW) mine[r * DW + d] = st.acc[x];
+                }
+                if (lane == 0) {
+                    sm_m[warp][r] = st.m;
+                    sm_l[warp][r] = st.l;
+                }
+                __syncwarp();
+            }
+            __syncthreads();
+            // four neighbouring dims of a row per thread and turn
+            for (int x = tid * 4; x < RW * DW; x += kFewThreads * 4) {
+                const int r = x / DW, d = part * DW + x % DW;
+                const FewRow fr = few_row(f, q, kv_head, group, r);
+                if (!fr.live) continue;
+                float M = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, sm_m[w][r]);
+                float L = 0.0f;
+                float4 s4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int w = 0; w < kFewWarps; ++w) {
+                    const float4 t = *reinterpret_cast<const float4*>(merge + w * 1024 + x);
+                    const float wt = sm_m[w][r] == -INFINITY ? 0.0f : fast_exp2(sm_m[w][r] - M);
+                    if (wt == 0.0f && sm_l[w][r] == 0.0f) continue;
+                    L = fmaf(wt, sm_l[w][r], L);
+                    s4.x = fmaf(wt, t.x, s4.x);
+                    s4.y = fmaf(wt, t.y, s4.y);
+                    s4.z = fmaf(wt, t.z, s4.z);
+                    s4.w = fmaf(wt, t.w, s4.w);
+                }
+                if (whole_item) {
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+                    const int64_t at = static_cast<int64_t>(fr.t) * f.a.heads + fr.h;
+                    uint2 y;
+                    if (L == 0.0f) s4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (f.a.out_type == AFX_F16)
+                        y = make_uint2(pack2_bits<AFX_F16>(s4.x * inv, s4.y * inv), pack2_bits<AFX_F16>(s4.z * inv, s4.w * inv));
+                    else
+                        y = make_uint2(pack2_bits<AFX_BF16>(s4.x * inv, s4.y * inv), pack2_bits<AFX_BF16>(s4.z * inv, s4.w * inv));
+                    *reinterpret_cast<uint2*>(f.a.out + at * D + d) = y;
+                    if (f.a.lse != nullptr && d == 0) f.a.lse[at] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                } else {
+                    *reinterpret_cast<float4*>(slot + 2 * kFewRows + r * D + d) = s4;
+                    if (d == 0) {
+                        slot[r] = M;
+                        slot[kFewRows + r] = L;
+                    }
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Joins what the ranges left unfinished, in the ranges' order; rows without any position get zeros.  A block per item.
+template <int D>
+__global__ void __launch_bounds__(kFewThreads) paged_join_kernel(PagedFewArgs f, int blocks, int max_items) {
+    __shared__ int64_t scratch[kFewThreads + kFewWarps];
+    __shared__ int64_t sh_before;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int b = blockIdx.x / max_items, item = blockIdx.x - b * max_items, tid = threadIdx.x;
+    const FewSeq q = few_seq(f, b, false);
+    if (item >= q.items) return;
+    const int groups = q.items / f.a.w.n_kv, kv_head = item / groups, group = item - kv_head * groups;
+    int r_lo = 0, r_hi = -1;
+    int64_t first_tile = 0, total = 0;
+    if (q.tiles > 0) {
+        total = few_list_total(f, scratch, false);
+        if (tid == 0) {
+            const int per = (f.a.w.n_seqs + kFewThreads - 1) / kFewThreads;
+            int64_t sum = scratch[b / per];
+            for (int i = b / per * per; i < b; ++i) {
+                const FewSeq o = few_seq(f, i, false);
+                sum += static_cast<int64_t>(o.tiles) * o.items;
+            }
+            sh_before = sum;
+        }
+        __syncthreads();
+        first_tile = sh_before + static_cast<int64_t>(item) * q.tiles;
+        const int64_t last_tile = first_tile + q.tiles - 1;
+        // range i holds tiles [total i / blocks, total (i + 1) / blocks)
+        r_lo = static_cast<int>(first_tile * blocks / total);
+        while (few_range(total, r_lo + 1, blocks) <= first_tile) ++r_lo;
+        while (few_range(total, r_lo, blocks) > first_tile) --r_lo;
+        r_hi = static_cast<int>(last_tile * blocks / total);
+        while (few_range(total, r_hi + 1, blocks) <= last_tile) ++r_hi;
+        while (few_range(total, r_hi, blocks) > last_tile) --r_hi;
+        if (r_lo == r_hi) return;  // one range: it is finished
+    }
+    for (int x = tid * 4; x < f.rows_per_group * D; x += kFewThreads * 4) {
+        const int r = x / D, d = x % D;
+        const FewRow fr = few_row(f, q, kv_head, group, r);
+        if (!fr.live) continue;
+        float M = -INFINITY, L = 0.0f;
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = r_lo; i <= r_hi; ++i) {
+            const int64_t lo = few_range(total, i, blocks);
+            if (lo == few_range(total, i + 1, blocks)) continue;  // an empty range
+            const bool first_piece = lo >= first_tile;            // the range starts in (or with) this item
+            const float* slot = f.slots + static_cast<int64_t>(2 * i + (first_piece ? 0 : 1)) * few_slot_floats(D);
+            const float m = slot[r], l = slot[kFewRows + r];
+            const float4 t = *reinterpret_cast<const float4*>(slot + 2 * kFewRows + r * D + d);
+            if (m == -INFINITY && l == 0.0f) continue;  // nothing seen there
+            const float mn = fmaxf(M, m), wa = M == -INFINITY ? 0.0f : fast_exp2(M - mn), wb = fast_exp2(m - mn);
+            M = mn;
+            L = fmaf(L, wa, l * wb);
+            s.x = fmaf(s.x, wa, t.x * wb);
+            s.y = fmaf(s.y, wa, t.y * wb);
+            s.z = fmaf(s.z, wa, t.z * wb);
+            s.w = fmaf(s.w, wa, t.w * wb);
+        }
+        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+        const int64_t at = static_cast<int64_t>(fr.t) * f.a.heads + fr.h;
+        uint2 y;
+        if (f.a.out_type == AFX_F16)
+            y = make_uint2(pack2_bits<AFX_F16>(s.x * inv, s.y * inv), pack2_bits<AFX_F16>(s.z * inv, s.w * inv));
+        else
+            y = make_uint2(pack2_bits<AFX_BF16>(s.x * inv, s.y * inv), pack2_bits<AFX_BF16>(s.z * inv, s.w * inv));
+        *reinterpret_cast<uint2*>(f.a.out + at * D + d) = y;
+        if (f.a.lse != nullptr && d == 0) f.a.lse[at] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+    }
+}
+
+}  // namespace afx
