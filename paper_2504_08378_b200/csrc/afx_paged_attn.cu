@@ -66,8 +66,7 @@ extern "C" size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_h
     afx::PagedAttnArgs a = {};
     if (afx::attn_args(kv, n_heads, nullptr, &a) != AFX_OK) return 0;
     if (kv->max_new > AFX_MAX_T) return 0;
-    const size_t bytes = static_cast<size_t>(2) * afx::kFewMaxBlocks * afx::few_slot_floats(kv->head_dim) * sizeof(float);
-    return (bytes + 255) / 256 * 256;
+    return (afx::few_workspace_bytes(kv->head_dim) + 255) / 256 * 256;
 }
 
 extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads,
@@ -103,7 +102,8 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
     if (kv->max_new <= AFX_MAX_T) {
         PagedFewArgs f = {};
         f.a = a;
-        f.slots = static_cast<float*>(workspace);
+        f.joins = static_cast<FewJoin*>(workspace);
+        f.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_slots_at());
         return launch_paged_few(kv->dtype, D, f, st);
     }
     if (D == 128)

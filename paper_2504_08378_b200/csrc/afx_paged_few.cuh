@@ -36,12 +36,28 @@ struct FewCfg {
     static constexpr int kDyn = kRing + kMerge;
 };
 
-// An unfinished item's sums in the workspace: slot 2 i is the first piece of range i, 2 i + 1 a later one.
-__host__ __device__ constexpr int few_slot_floats(int D) { return kFewRows * (D + 2); }  // m[16], l[16], acc[16][D]
+// What an item costs beside its tiles (queries, the warps' sums), in tiles: the ranges are cut with it counted in.
+constexpr int kFewItemCost = 1;
+
+// The workspace: a descriptor per range, then slots of an unfinished item's sums (m[16], l[16], acc[16][D]).  Slot 2 i is
+// the piece that range i begins with where the item began in an earlier range, 2 i + 1 the piece of the item that begins in
+// range i and ends in a later one (the descriptor of range i tells which).
+struct FewJoin {
+    int32_t last;             // range in which the item ends; < 0: none
+    int32_t row0, h0;         // the sequence's first token row, the kv head's first query head
+    int32_t first, rows;      // rows first .. first + rows - 1 of (token, query head of the kv head)
+    int32_t pad[3];
+};
+__host__ __device__ constexpr int few_slot_floats(int D) { return kFewRows * (D + 2); }
+__host__ __device__ constexpr size_t few_slots_at() { return kFewMaxBlocks * sizeof(FewJoin); }
+__host__ __device__ constexpr size_t few_workspace_bytes(int D) {
+    return few_slots_at() + static_cast<size_t>(2) * kFewMaxBlocks * few_slot_floats(D) * sizeof(float);
+}
 
 struct PagedFewArgs {
     PagedAttnArgs a;
     int rows_per_group;  // 8 (packed) or 16
+    FewJoin* joins;
     float* slots;
 };
 
@@ -68,81 +84,102 @@ __device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool rep
     return q;
 }
 
-// The list's length; scratch[i] = tiles in front of the sequences of thread i (kFewThreads + kFewWarps values).  All threads call it.
-__device__ __forceinline__ int64_t few_list_total(const PagedFewArgs& f, int64_t* scratch, bool report) {
+// Where a range begins in the list (units: tiles, and kFewItemCost in front of an item's).
+struct FewStart {
+    int64_t before;  // units in front of the sequence
+    int b;
+};
+struct FewScratch {
+    int64_t warp_units[kFewWarps];
+    FewStart start;
+};
+// The list's length.  All threads of the block call it.
+__device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* sc, bool report, int64_t& mine_before, int64_t& mine) {
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads, tid = threadIdx.x;
-    int64_t mine = 0;
+    mine = 0;
     for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
         const FewSeq q = few_seq(f, i, report);
-        mine += static_cast<int64_t>(q.tiles) * q.items;
+        mine += static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
     }
-    // inclusive sums over the threads
     int64_t incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
         if (lane_id() >= o) incl += up;
     }
-    if (lane_id() == 31) scratch[kFewThreads + warp_id()] = incl;
-    __syncthreads();
-    int64_t base = 0;
-    for (int w = 0; w < warp_id(); ++w) base += scratch[kFewThreads + w];
-    scratch[tid] = base + incl - mine;  // tiles in front of this thread's sequences
+    if (lane_id() == 31) sc->warp_units[warp_id()] = incl;
     __syncthreads();
     int64_t total = 0;
-    for (int w = 0; w < kFewWarps; ++w) total += scratch[kFewThreads + w];
+    mine_before = incl - mine;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) {
+        if (w < warp_id()) mine_before += sc->warp_units[w];
+        total += sc->warp_units[w];
+    }
     return total;
 }
-// The sequence that holds tile `at` (0 <= at < total) and the tiles in front of it; one thread's work, from scratch.
-__device__ __forceinline__ int few_find(const PagedFewArgs& f, const int64_t* scratch, int64_t at, int64_t& before) {
+// The thread among whose sequences unit `at` lies writes down which.
+__device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int64_t mine_before, int64_t mine) {
+    if (at < mine_before || at >= mine_before + mine) return;
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads;
-    int lo = 0, hi = kFewThreads - 1;
-    while (lo < hi) {  // the last thread whose sequences start at or before the tile
-        const int mid = (lo + hi + 1) >> 1;
-        if (scratch[mid] <= at) lo = mid; else hi = mid - 1;
-    }
-    int64_t sum = scratch[lo];
-    int b = lo * per;
-    for (; b < min(n, (lo + 1) * per) - 1; ++b) {
+    int b = threadIdx.x * per;
+    for (; b < min(n, static_cast<int>(threadIdx.x + 1) * per) - 1; ++b) {
         const FewSeq q = few_seq(f, b, false);
-        const int64_t t = static_cast<int64_t>(q.tiles) * q.items;
-        if (sum + t > at) break;
-        sum += t;
+        const int64_t t = static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
+        if (mine_before + t > at) break;
+        mine_before += t;
     }
-    before = sum;
-    return b;
+    sc->start = {mine_before, b};
 }
-__device__ __forceinline__ int64_t few_range(int64_t total, int i, int blocks) { return total * i / blocks; }
+// Range i holds units [i per + min(i, rest), ..): the first `rest` ranges one more.
+struct FewRanges {
+    int64_t per;
+    int rest, n;
+    __device__ __forceinline__ FewRanges(int64_t total, int blocks) {
+        n = static_cast<int>(min(static_cast<int64_t>(blocks), total));
+        per = n > 0 ? total / n : 0;
+        rest = n > 0 ? static_cast<int>(total - per * n) : 0;
+    }
+    __device__ __forceinline__ int64_t begin(int i) const { return per * i + min(i, rest); }
+    __device__ __forceinline__ int of(int64_t unit) const {
+        const int64_t wide = (per + 1) * rest;
+        return static_cast<int>(unit < wide ? unit / (per + 1) : rest + (unit - wide) / per);
+    }
+};
 
 // A block's walk over its range: the pieces of items in it, one after the other.
 struct FewWalk {
     FewSeq q;
     int b, item;
     int t0, t1;         // this piece's tiles of the item
-    int64_t left;       // tiles of the range behind this piece
+    int64_t left;       // units of the range behind this piece
     bool more;          // there is a piece
 
-    __device__ __forceinline__ void cut() {
-        t1 = static_cast<int>(min(static_cast<int64_t>(q.tiles), t0 + left));
-        left -= t1 - t0;
+    // The piece from unit u0 of the item on; false where the range ends in front of its tiles.
+    __device__ __forceinline__ bool cut(int u0) {
+        const int u1 = static_cast<int>(min(static_cast<int64_t>(q.tiles + kFewItemCost), u0 + left));
+        left -= u1 - u0;
+        t0 = max(u0 - kFewItemCost, 0);
+        t1 = max(u1 - kFewItemCost, 0);
+        return t1 > t0 || q.tiles == 0;
     }
     __device__ __forceinline__ void next(const PagedFewArgs& f) {
-        if (left <= 0) {
-            more = false;
-            return;
-        }
-        t0 = 0;
-        if (++item == q.items) {
-            item = 0;
-            do {
-                if (++b >= f.a.w.n_seqs) {  // (lengths that changed under the call)
-                    more = false;
-                    return;
-                }
-                q = few_seq(f, b, false);
-            } while (q.tiles == 0 || q.items == 0);
-        }
-        cut();
+        do {
+            if (left <= 0) {
+                more = false;
+                return;
+            }
+            if (++item >= q.items) {
+                item = 0;
+                do {
+                    if (++b >= f.a.w.n_seqs) {  // (lengths that changed under the call)
+                        more = false;
+                        return;
+                    }
+                    q = few_seq(f, b, false);
+                } while (q.items == 0);
+            }
+        } while (!cut(0));
     }
     // chunks of this piece that warp w takes: w, w + warps, ..
     __device__ __forceinline__ int chunks(int w) const {
@@ -202,6 +239,22 @@ __device__ __forceinline__ bool few_sees(const PagedMask& m, int pos, int p) {
     return p <= pos && (m.window == 0 || p > pos - m.window || p < m.sinks);
 }
 
+// Four dims of a finished row; nothing seen: zeros.
+template <int D>
+__device__ __forceinline__ void few_store(const PagedFewArgs& f, int t, int h, int d, const float4& s, float M, float L) {
+    const bool none = L == 0.0f;
+    const float inv = 1.0f / L;
+    const float4 v = none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+    const int64_t at = static_cast<int64_t>(t) * f.a.heads + h;
+    uint2 y;
+    if (f.a.out_type == AFX_F16)
+        y = make_uint2(pack2_bits<AFX_F16>(v.x, v.y), pack2_bits<AFX_F16>(v.z, v.w));
+    else
+        y = make_uint2(pack2_bits<AFX_BF16>(v.x, v.y), pack2_bits<AFX_BF16>(v.z, v.w));
+    *reinterpret_cast<uint2*>(f.a.out + at * D + d) = y;
+    if (f.a.lse != nullptr && d == 0) f.a.lse[at] = none ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
 template <int D, int CT, bool PACK, bool QF32>
 __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs f) {
     using Cfg = FewCfg<D>;
@@ -211,44 +264,58 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
     extern __shared__ __align__(128) unsigned char dyn[];
     __shared__ uint32_t stage_mask[kFewWarps][ST];
     __shared__ float sm_m[kFewWarps][kFewRows], sm_l[kFewWarps][kFewRows];
-    __shared__ int64_t start_before;
-    __shared__ int start_b;
+    __shared__ FewScratch scratch;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
     float* merge = reinterpret_cast<float*>(dyn + Cfg::kRing);
-    int64_t* scratch = reinterpret_cast<int64_t*>(merge);  // (before the first merge)
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dyn)) + warp * ST * Cfg::kChunkBytes;
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const int64_t total = few_list_total(f, scratch, blockIdx.x == 0);
-    const int64_t lo = few_range(total, blockIdx.x, gridDim.x), hi = few_range(total, blockIdx.x + 1, gridDim.x);
-    if (lo >= hi) return;
-    if (tid == 0) {
-        int64_t before;
-        start_b = few_find(f, scratch, lo, before);
-        start_before = before;
-    }
+    int64_t mine_before, mine;
+    const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine);
+    const FewRanges ranges(total, gridDim.x);
+    const int my = blockIdx.x;
+    if (tid == 0) f.joins[my].last = -1;  // (a later piece may say otherwise)
+    if (my >= ranges.n) return;
+    const int64_t lo = ranges.begin(my), hi = ranges.begin(my + 1);
+    few_find(f, &scratch, lo, mine_before, mine);
     __syncthreads();
     FewWalk con;
-    con.b = start_b;
+    con.b = scratch.start.b;
     con.q = few_seq(f, con.b, false);
-    con.item = static_cast<int>((lo - start_before) / con.q.tiles);
-    con.t0 = static_cast<int>((lo - start_before) - static_cast<int64_t>(con.item) * con.q.tiles);
-    con.left = hi - lo;
-    con.more = true;
-    con.cut();
+    {
+        const int64_t u = lo - scratch.start.before;
+        const int per_item = con.q.tiles + kFewItemCost;
+        con.item = static_cast<int>(u / per_item);
+        con.left = hi - lo;
+        con.more = true;
+        if (!con.cut(static_cast<int>(u - static_cast<int64_t>(con.item) * per_item))) con.next(f);
+    }
 
     // ---- the ring's filling side: chunk after chunk of this warp, across pieces
     FewWalk pro = con;
-    int pk = 0, pn = pro.chunks(warp), p_stage = 0;
+    int pk = 0, pn = pro.more ? pro.chunks(warp) : 0, p_stage = 0;
     int64_t p_off = -1;  // lane j < 16: offset of the next chunk's position j; -1: leave out
+    // the item's query rows into L1, a line of 128 bytes per lane: they are wanted as soon as its first chunk is there
+    auto warm_queries = [&](const FewWalk& w) {
+        constexpr int LINES = D * (QF32 ? 4 : 2) / 128;
+        const int groups = w.q.items / f.a.w.n_kv, kv_head = w.item / groups;
+        for (int x = lane; x < (PACK ? 8 : 16) * LINES; x += 32) {
+            const FewRow r = few_row(f, w.q, kv_head, w.item - kv_head * groups, x / LINES);
+            if (r.live) {
+                const char* at = f.a.q + (r.t * f.a.ldq + static_cast<int64_t>(r.h) * D) * (QF32 ? 4 : 2) + x % LINES * 128;
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(at));
+            }
+        }
+    };
     auto look_up = [&]() {
         while (pro.more && pk >= pn) {
             pro.next(f);
             pk = 0;
             pn = pro.more ? pro.chunks(warp) : 0;
+            if (pro.more) warm_queries(pro);
         }
         if (!pro.more) return;
         const int v = pro.t0 * kFewTile + (pk * kFewWarps + warp) * kFewChunk + (lane & 15);
@@ -285,8 +352,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
     for (int i = 0; i < ST - 1; ++i) issue();
 
     int stage = 0;
-    bool first_piece = true;
-    for (; con.more; con.next(f), first_piece = false) {
+    for (; con.more; con.next(f)) {
         const FewSeq& q = con.q;
         const int groups = q.items / f.a.w.n_kv, kv_head = con.item / groups, group = con.item - kv_head * groups;
         // ---- queries of the lane's rows as fragments of the first product
@@ -480,7 +546,18 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
             }
         }
         const bool whole_item = con.t0 == 0 && con.t1 == q.tiles;
-        float* slot = f.slots + static_cast<int64_t>(2 * blockIdx.x + (first_piece ? 0 : 1)) * few_slot_floats(D);
+        float* slot = f.slots + static_cast<int64_t>(2 * my + (con.t0 > 0 ? 0 : 1)) * few_slot_floats(D);
+        if (!whole_item && con.t0 == 0 && tid == 0) {  // this range has the item joined
+            const int64_t end = hi + (q.tiles - con.t1);   // (its piece ends the range)
+            const int first = group * f.rows_per_group;
+            FewJoin j = {};
+            j.last = ranges.of(end - 1);
+            j.row0 = q.s.row0;
+            j.h0 = kv_head * f.a.rep;
+            j.first = first;
+            j.rows = min(f.rows_per_group, q.s.n * f.a.rep - first);
+            f.joins[my] = j;
+        }
         // 1024 values of a warp at a time: 8 rows x 128 dims, 16 rows x 64 dims (twice), 8 rows x 64 dims
         constexpr int RW = PACK ? 8 : 16, DW = PACK ? D : 64;
 #pragma unroll
@@ -545,16 +622,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                     s4.w = fmaf(wt, t.w, s4.w);
                 }
                 if (whole_item) {
-                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    const int64_t at = static_cast<int64_t>(fr.t) * f.a.heads + fr.h;
-                    uint2 y;
-                    if (L == 0.0f) s4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (f.a.out_type == AFX_F16)
-                        y = make_uint2(pack2_bits<AFX_F16>(s4.x * inv, s4.y * inv), pack2_bits<AFX_F16>(s4.z * inv, s4.w * inv));
-                    else
-                        y = make_uint2(pack2_bits<AFX_BF16>(s4.x * inv, s4.y * inv), pack2_bits<AFX_BF16>(s4.z * inv, s4.w * inv));
-                    *reinterpret_cast<uint2*>(f.a.out + at * D + d) = y;
-                    if (f.a.lse != nullptr && d == 0) f.a.lse[at] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                    few_store<D>(f, fr.t, fr.h, d, s4, M, L);
                 } else {
                     *reinterpret_cast<float4*>(slot + 2 * kFewRows + r * D + d) = s4;
                     if (d == 0) {
@@ -568,74 +636,42 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
     }
 }
 
-// Joins what the ranges left unfinished, in the ranges' order; rows without any position get zeros.  A block per item.
+// Joins what the ranges left unfinished, in the ranges' order: grid (ranges, pieces of 512 values of an item).
 template <int D>
-__global__ void __launch_bounds__(kFewThreads) paged_join_kernel(PagedFewArgs f, int blocks, int max_items) {
-    __shared__ int64_t scratch[kFewThreads + kFewWarps];
-    __shared__ int64_t sh_before;
+__global__ void __launch_bounds__(kFewThreads) paged_join_kernel(PagedFewArgs f) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int b = blockIdx.x / max_items, item = blockIdx.x - b * max_items, tid = threadIdx.x;
-    const FewSeq q = few_seq(f, b, false);
-    if (item >= q.items) return;
-    const int groups = q.items / f.a.w.n_kv, kv_head = item / groups, group = item - kv_head * groups;
-    int r_lo = 0, r_hi = -1;
-    int64_t first_tile = 0, total = 0;
-    if (q.tiles > 0) {
-        total = few_list_total(f, scratch, false);
-        if (tid == 0) {
-            const int per = (f.a.w.n_seqs + kFewThreads - 1) / kFewThreads;
-            int64_t sum = scratch[b / per];
-            for (int i = b / per * per; i < b; ++i) {
-                const FewSeq o = few_seq(f, i, false);
-                sum += static_cast<int64_t>(o.tiles) * o.items;
-            }
-            sh_before = sum;
+    const FewJoin j = f.joins[blockIdx.x];
+    const int x = (static_cast<int>(blockIdx.y) * kFewThreads + static_cast<int>(threadIdx.x)) * 4, r = x / D, d = x % D;
+    if (j.last < 0 || r >= j.rows) return;
+    float M = -INFINITY, L = 0.0f;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    constexpr int U = 8;  // pieces on their way at once
+    for (int i0 = blockIdx.x; i0 <= j.last; i0 += U) {
+        float m[U], l[U];
+        float4 t[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = min(i0 + u, j.last);
+            const float* slot = f.slots + static_cast<int64_t>(2 * i + (i == static_cast<int>(blockIdx.x) ? 1 : 0)) * few_slot_floats(D);
+            m[u] = slot[r];
+            l[u] = slot[kFewRows + r];
+            t[u] = *reinterpret_cast<const float4*>(slot + 2 * kFewRows + r * D + d);
         }
-        __syncthreads();
-        first_tile = sh_before + static_cast<int64_t>(item) * q.tiles;
-        const int64_t last_tile = first_tile + q.tiles - 1;
-        // range i holds tiles [total i / blocks, total (i + 1) / blocks)
-        r_lo = static_cast<int>(first_tile * blocks / total);
-        while (few_range(total, r_lo + 1, blocks) <= first_tile) ++r_lo;
-        while (few_range(total, r_lo, blocks) > first_tile) --r_lo;
-        r_hi = static_cast<int>(last_tile * blocks / total);
-        while (few_range(total, r_hi + 1, blocks) <= last_tile) ++r_hi;
-        while (few_range(total, r_hi, blocks) > last_tile) --r_hi;
-        if (r_lo == r_hi) return;  // one range: it is finished
-    }
-    for (int x = tid * 4; x < f.rows_per_group * D; x += kFewThreads * 4) {
-        const int r = x / D, d = x % D;
-        const FewRow fr = few_row(f, q, kv_head, group, r);
-        if (!fr.live) continue;
-        float M = -INFINITY, L = 0.0f;
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int i = r_lo; i <= r_hi; ++i) {
-            const int64_t lo = few_range(total, i, blocks);
-            if (lo == few_range(total, i + 1, blocks)) continue;  // an empty range
-            const bool first_piece = lo >= first_tile;            // the range starts in (or with) this item
-            const float* slot = f.slots + static_cast<int64_t>(2 * i + (first_piece ? 0 : 1)) * few_slot_floats(D);
-            const float m = slot[r], l = slot[kFewRows + r];
-            const float4 t = *reinterpret_cast<const float4*>(slot + 2 * kFewRows + r * D + d);
-            if (m == -INFINITY && l == 0.0f) continue;  // nothing seen there
-            const float mn = fmaxf(M, m), wa = M == -INFINITY ? 0.0f : fast_exp2(M - mn), wb = fast_exp2(m - mn);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u > j.last || (m[u] == -INFINITY && l[u] == 0.0f)) continue;  // (nothing seen there)
+            const float mn = fmaxf(M, m[u]), wa = M == -INFINITY ? 0.0f : fast_exp2(M - mn), wb = fast_exp2(m[u] - mn);
             M = mn;
-            L = fmaf(L, wa, l * wb);
-            s.x = fmaf(s.x, wa, t.x * wb);
-            s.y = fmaf(s.y, wa, t.y * wb);
-            s.z = fmaf(s.z, wa, t.z * wb);
-            s.w = fmaf(s.w, wa, t.w * wb);
+            L = fmaf(L, wa, l[u] * wb);
+            s.x = fmaf(s.x, wa, t[u].x * wb);
+            s.y = fmaf(s.y, wa, t[u].y * wb);
+            s.z = fmaf(s.z, wa, t[u].z * wb);
+            s.w = fmaf(s.w, wa, t[u].w * wb);
         }
-        const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-        const int64_t at = static_cast<int64_t>(fr.t) * f.a.heads + fr.h;
-        uint2 y;
-        if (f.a.out_type == AFX_F16)
-            y = make_uint2(pack2_bits<AFX_F16>(s.x * inv, s.y * inv), pack2_bits<AFX_F16>(s.z * inv, s.w * inv));
-        else
-            y = make_uint2(pack2_bits<AFX_BF16>(s.x * inv, s.y * inv), pack2_bits<AFX_BF16>(s.z * inv, s.w * inv));
-        *reinterpret_cast<uint2*>(f.a.out + at * D + d) = y;
-        if (f.a.lse != nullptr && d == 0) f.a.lse[at] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
     }
+    const int rr = j.first + r, i = rr / f.a.rep;
+    few_store<D>(f, j.row0 + i, j.h0 + rr - i * f.a.rep, d, s, M, L);
 }
 
 }  // namespace afx
