@@ -1,60 +1,14 @@
 // afx_paged_attn: checks and the choice of the kernel.
 #include "afx_paged_few.cuh"
+#include "afx_paged_prompt.cuh"
 
 namespace afx {
-
-// One warp per (token row, query head), positions one after the other.
-template <int D, int CT>
-__global__ void __launch_bounds__(128) paged_rows_kernel(PagedAttnArgs a) {
-    constexpr int E = D / 32;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int b = blockIdx.z, lane = lane_id();
-    const int h = blockIdx.x * 4 + warp_id();
-    const SeqSpan s = paged_span(a.w, b, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
-    if (h >= a.heads) return;
-    for (int i = blockIdx.y; i < s.n; i += gridDim.y) {
-        const int p = s.first + i, t = s.row0 + i, g = h / a.rep;
-        float q[E];
-        for (int e = 0; e < E; ++e)
-            q[e] = a.scale * typed_value(a.q, a.q_type, t * a.ldq + static_cast<int64_t>(h) * D + lane * E + e);
-        RowState<D> st;
-        for (int e = 0; e < E; ++e) st.acc[e] = 0.0f;
-        if (p >= 0) {
-            const int low = paged_low(a.mask, p);
-            attend_row<D, CT>(a.w, b, g, q, 0, paged_few(a.mask, low), st);
-            attend_row<D, CT>(a.w, b, g, q, low, p + 1, st);
-        }
-        const int64_t at = static_cast<int64_t>(t) * a.heads + h;
-        for (int e = 0; e < E; ++e)
-            a.out[at * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
-        if (a.lse != nullptr && lane == 0) a.lse[at] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
-    }
-}
-
-template <int D, int CT>
-static afx_status launch_rows(const PagedAttnArgs& a, cudaStream_t st) {
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((a.heads + 3) / 4, a.w.max_new < 65535 ? a.w.max_new : 65535, a.w.n_seqs);
-    cfg.blockDim = dim3(128);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, paged_rows_kernel<D, CT>, a) != cudaSuccess) {
-        cudaGetLastError();
-        return AFX_ERR_CUDA;
-    }
-    return AFX_OK;
-}
 
 static afx_status attn_args(const afx_paged_kv* kv, int n_heads, int32_t* dev_status, PagedAttnArgs* a) {
     const afx_status rc = paged_view(kv, dev_status, &a->w);
     if (rc != AFX_OK) return rc;
     if (n_heads < 1 || n_heads % kv->n_kv_heads != 0) return AFX_ERR_INVALID_ARG;
-    if (n_heads > 8192) return AFX_ERR_CAPACITY;
+    if (n_heads > 8192 || static_cast<int64_t>(kv->n_tokens) * n_heads > 0x7FFFFFFF) return AFX_ERR_CAPACITY;
     a->heads = n_heads;
     a->rep = n_heads / kv->n_kv_heads;
     return AFX_OK;
@@ -106,7 +60,5 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
         f.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_slots_at());
         return launch_paged_few(kv->dtype, D, f, st);
     }
-    if (D == 128)
-        return kv->dtype == AFX_F16 ? launch_rows<128, AFX_F16>(a, st) : launch_rows<128, AFX_BF16>(a, st);
-    return kv->dtype == AFX_F16 ? launch_rows<64, AFX_F16>(a, st) : launch_rows<64, AFX_BF16>(a, st);
+    return launch_paged_prompt(kv->dtype, D, a, st);
 }

@@ -1,0 +1,447 @@
+// Attention of many new tokens per sequence (prompts, chunks of them) over the paged cache, on the 5th-generation
+// tensor cores.
+//
+// A block takes two tiles of 128 rows of one (sequence, kv head) -- rows are (token, query head of the kv head), so that heads which share
+// keys share their loads -- and walks the positions that their tokens see in tiles of 128.  Per tile of positions
+// and of rows:
+//   S = Q K^T    128 x 128 x D, both operands in shared memory, S in tensor memory
+//   P = 2^(S scale - m)   a thread per row: S out of tensor memory, P (16 bits) back into S's place
+//   O += P V     128 x D x 128, P from tensor memory, V from shared memory as it lies in the cache, O in tensor memory
+// One thread issues the products, of the two row tiles in turn: while one tile's P is computed the tensor cores
+// work for the other.  O is rescaled only when a row's maximum has grown by 2^8 since the last time (P stays
+// below 2^8; fp16 P is carried times 2^7, so that what is lost below its range is 2^-32 of the largest weight).
+// P is rounded to the cache's type (half a step of 2^-9 / 2^-12 relative per weight, averaged over the weights; the sums
+// of weights are taken before that rounding): 16-bit operands are what the tensor cores multiply at full rate.
+// Three warps fetch keys and values with cp.async, rows by way of the page table, any page size.
+//
+// Bound by the exponentials and the products alike: 2 x 128 x 128 exponentials are 2048 cycles of an SM's 16 per cycle, the four products
+// 2048 cycles at D = 128.
+#pragma once
+
+#include "afx_paged_attn.cuh"
+#include "afx_tcgen05.cuh"
+
+namespace afx {
+
+constexpr int kPrThreads = 384;  // warps 0-3: rows of tile 0, 4-7: tile 1, 8: products, 9-11: loads
+constexpr int kPrRows = 128, kPrTiles = 2, kPrPos = 128;
+constexpr int kPrLoaders = 3;
+constexpr float kPrGrow = 8.0f;  // powers of two that a row's maximum may grow by before O is rescaled
+
+afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, cudaStream_t st);  // afx_paged_prompt.cu
+
+template <int D>
+struct PrCfg {
+    static constexpr int kStages = D == 128 ? 2 : 3;
+    static constexpr int kBlock = kPrPos * 128;        // bytes of 128 rows of 64 values
+    static constexpr int kTile = kBlock * (D / 64);    // bytes of 128 rows of D values
+    static constexpr int kQ = 0, kK = kPrTiles * kTile, kV = kK + kStages * kTile;
+    static constexpr int kDyn = kV + kStages * kTile + 1024;  // (base rounded up to 1024)
+};
+
+struct PrBarriers {
+    uint64_t q_full, k_full[3], k_empty[3], v_full[3], v_empty[3], s_full[2], p_full[2], o_full[2], drain;
+};
+
+// What a block works on.
+struct PrWork {
+    SeqSpan s;
+    int b, kv_head, row_base;  // first of its 256 rows
+    int few, low;              // positions: [0, few), then low ..
+    int tiles[2];              // tiles of positions that each row tile sees
+};
+
+__device__ __forceinline__ int pr_row_tiles(const PagedAttnArgs& a, const SeqSpan& s) {
+    return static_cast<int>((static_cast<int64_t>(s.n) * a.rep + kPrTiles * kPrRows - 1) / (kPrTiles * kPrRows));
+}
+
+template <int D, int CT>
+__global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnArgs a) {
+    using Cfg = PrCfg<D>;
+    constexpr int ST = Cfg::kStages;
+    constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
+    extern __shared__ unsigned char dyn_raw[];
+    __shared__ PrBarriers bar;
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    __shared__ PrWork work;
+    __shared__ int warp_tiles[kPrThreads / 32];
+    __shared__ __align__(16) uint16_t page_ok[4][8];  // per tile of positions (mod 4) and 16 of them: the cache has them
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t base = smem_u32(dyn);
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- which rows: blocks go through the sequences' pairs of row tiles, kv heads side by side, later rows (with more
+    // positions) first within a sequence
+    const int pair = blockIdx.x / a.w.n_kv;
+    if (tid == 0) work.b = -1;
+    {
+        const int n = a.w.n_seqs, per = (n + kPrThreads - 1) / kPrThreads;
+        int mine = 0;
+        for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += pr_row_tiles(a, paged_span(a.w, i, blockIdx.x == 0));
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 31) warp_tiles[warp] = incl;
+        __syncthreads();
+        int before = incl - mine;
+        for (int w = 0; w < warp; ++w) before += warp_tiles[w];
+        if (pair >= before && pair < before + mine) {
+            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
+                const SeqSpan s = paged_span(a.w, i, false);
+                const int t = pr_row_tiles(a, s);
+                if (pair < before + t) {
+                    PrWork w;
+                    w.s = s;
+                    w.b = i;
+                    w.kv_head = blockIdx.x % a.w.n_kv;
+                    w.row_base = (t - 1 - (pair - before)) * kPrTiles * kPrRows;
+                    const int rows = s.n * a.rep;
+                    const int first = max(s.first + w.row_base / a.rep, 0);
+                    w.low = paged_low(a.mask, first);
+                    w.few = paged_few(a.mask, w.low);
+                    for (int x = 0; x < kPrTiles; ++x) {
+                        const int r0 = w.row_base + x * kPrRows, r1 = min(r0 + kPrRows, rows) - 1;
+                        const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
+                        w.tiles[x] = last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 0;
+                    }
+                    work = w;
+                    break;
+                }
+                before += t;
+            }
+        }
+    }
+    if (tid == 0) {
+        gave_up = 0;
+        mbar_init(&bar.q_full, kPrLoaders);
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(&bar.k_full[i], kPrLoaders);
+            mbar_init(&bar.v_full[i], kPrLoaders);
+            mbar_init(&bar.k_empty[i], 1);
+            mbar_init(&bar.v_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bar.s_full[i], 1);
+            mbar_init(&bar.p_full[i], 4);
+            mbar_init(&bar.o_full[i], 1);
+        }
+        mbar_init(&bar.drain, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (work.b < 0) return;  // (the grid is an upper bound; the same for all threads)
+    if (warp == 8) tmem_alloc(&tmem_at, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_at;
+    const PrWork w = work;
+    const int n_tiles = max(w.tiles[0], w.tiles[1]);
+    const int rows = w.s.n * a.rep;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8) {
+            // ---- products: one thread
+            if (lane == 0 && n_tiles > 0) {
+                constexpr uint32_t s_desc = mma_desc(CT == AFX_BF16, 128, kPrPos, false);
+                constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
+                bool ok = mbar_wait(&bar.q_full, 0, &gave_up);
+                auto scores = [&](int x, int j) {
+                    const uint32_t q = base + Cfg::kQ + x * Cfg::kTile, k = base + Cfg::kK + (j % ST) * Cfg::kTile;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (i / 4) * Cfg::kBlock + (i % 4) * 32;
+                        tc_mma_ss(tmem + x * kPrPos, smem_desc(q + off, 16), smem_desc(k + off, 16), s_desc, i > 0);
+                    }
+                    tc_commit(&bar.s_full[x]);
+                };
+                ok = ok && mbar_wait(&bar.k_full[0], 0, &gave_up);
+                tc_fence_after();
+                if (ok) {
+                    for (int x = 0; x < 2; ++x)
+                        if (w.tiles[x] > 0) scores(x, 0);
+                    tc_commit(&bar.k_empty[0]);
+                }
+                for (int j = 0; ok && j < n_tiles; ++j) {
+                    ok = mbar_wait(&bar.v_full[j % ST], (j / ST) & 1, &gave_up);
+                    if (ok && j + 1 < n_tiles) ok = mbar_wait(&bar.k_full[(j + 1) % ST], ((j + 1) / ST) & 1, &gave_up);
+                    for (int x = 0; ok && x < 2; ++x) {
+                        if (j >= w.tiles[x]) continue;
+                        ok = mbar_wait(&bar.p_full[x], j & 1, &gave_up);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t v = base + Cfg::kV + (j % ST) * Cfg::kTile;
+#pragma unroll
+                        for (int i = 0; i < kPrPos / 16; ++i)
+                            tc_mma_ts(tmem + 256 + x * D, tmem + x * kPrPos + i * 8, smem_desc(v + i * 2048, Cfg::kBlock), o_desc, j > 0 || i > 0);
+                        if (j + 1 < w.tiles[x])
+                            scores(x, j + 1);
+                        else
+                            tc_commit(&bar.o_full[x]);
+                    }
+                    if (ok) {
+                        tc_commit(&bar.v_empty[j % ST]);
+                        if (j + 1 < n_tiles) tc_commit(&bar.k_empty[(j + 1) % ST]);
+                    }
+                }
+                if (!ok) {  // what has been issued ends before tensor memory is given back
+                    int alone = 0;
+                    report_status(a.w.status, AFX_ERR_TIMEOUT);
+                    tc_commit(&bar.drain);
+                    mbar_wait(&bar.drain, 0, &alone);
+                }
+            }
+            __syncwarp();
+        } else {
+            // ---- loads: blocks of 16 rows; a lane of the first 16 looks one row up, 16 (or 8) lanes copy a row
+            constexpr int PIECES = D / 8, RPI = 32 / PIECES;
+            const int lw = warp - 9;
+            auto put = [&](uint32_t tile, int row, int piece, const void* src, int bytes) {
+                const uint32_t at = tile + (piece >> 3) * Cfg::kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(src), "r"(bytes) : "memory");
+            };
+            auto done = [&](uint64_t* full) {  // (after the wait for the copies)
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full);
+            };
+            for (int r0 = lw * RPI; r0 < kPrTiles * kPrRows; r0 += kPrLoaders * RPI) {
+                const int r = r0 + lane / PIECES, rr = w.row_base + r, piece = lane % PIECES;
+                const int i = rr / a.rep;
+                const bool live = rr < rows;
+                const int64_t at = live ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D + piece * 8 : 0;
+                put(base + Cfg::kQ + (r / kPrRows) * Cfg::kTile, r % kPrRows, piece, reinterpret_cast<const uint16_t*>(a.q) + at, live ? 16 : 0);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            const int nv = max(w.tiles[0], w.tiles[1]) * kPrPos;  // (rows behind the last visible position are left out below)
+            const int end = min(w.s.len, w.s.first + w.s.n);
+            int64_t off[3], next[3];
+            auto look_up = [&](int j) {
+#pragma unroll
+                for (int x = 0; x < 3; ++x) {
+                    const int v = j * kPrPos + (lw + x * kPrLoaders) * 16 + (lane & 15);
+                    const int p = v < w.few ? v : v - w.few + w.low;
+                    next[x] = -1;
+                    if (lw + x * kPrLoaders < 8 && v < nv && p < end) {
+                        next[x] = paged_row(a.w, w.b, p, w.kv_head);
+                        if (next[x] < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
+                    }
+                }
+            };
+            auto fill = [&](const uint16_t* pages, uint32_t tile) {
+#pragma unroll
+                for (int x = 0; x < 3; ++x) {
+                    const int blk = lw + x * kPrLoaders;
+                    if (blk >= 8) continue;
+#pragma unroll
+                    for (int i = 0; i < 16 / RPI; ++i) {
+                        const int row = i * RPI + lane / PIECES, piece = lane % PIECES;
+                        const int64_t o = __shfl_sync(0xFFFFFFFFu, off[x], row);
+                        put(tile, blk * 16 + row, piece, pages + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            bool ok = true;
+            look_up(0);
+            // loads in the order Q, K0, V0, K1, V1, ..; three of them on their way, each reported when it has landed
+            for (int j = 0; ok && j < n_tiles; ++j) {
+                const int st = j % ST;
+                const uint32_t free_parity = ((j / ST) & 1) ^ 1;
+#pragma unroll
+                for (int x = 0; x < 3; ++x) off[x] = next[x];
+                if (j + 1 < n_tiles) look_up(j + 1);
+                if (j >= ST) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.k_empty[st], free_parity, &gave_up));
+                if (!ok) break;
+#pragma unroll
+                for (int x = 0; x < 3; ++x) {
+                    const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
+                    if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 3][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                }
+                fill(a.w.k, base + Cfg::kK + st * Cfg::kTile);
+                if (j > 0) {
+                    asm volatile("cp.async.wait_group 2;" ::: "memory");
+                    done(&bar.k_full[(j - 1) % ST]);
+                }
+                if (j >= ST) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.v_empty[st], free_parity, &gave_up));
+                if (!ok) break;
+                fill(a.w.v, base + Cfg::kV + st * Cfg::kTile);
+                asm volatile("cp.async.wait_group 2;" ::: "memory");
+                done(j == 0 ? &bar.q_full : &bar.v_full[(j - 1) % ST]);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (ok && n_tiles > 0) {
+                done(&bar.k_full[(n_tiles - 1) % ST]);
+                done(&bar.v_full[(n_tiles - 1) % ST]);
+            } else if (!ok && lane == 0) {
+                report_status(a.w.status, AFX_ERR_TIMEOUT);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        // ---- softmax: a thread per row
+        const int x = warp >> 2, r = (warp & 3) * 32 + lane, rr = w.row_base + x * kPrRows + r;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lanes + x * kPrPos, o_at = tmem + lanes + 256 + x * D;
+        const int i = rr / a.rep, h = w.kv_head * a.rep + rr - i * a.rep;
+        const bool live = rr < rows;
+        const int pos = live ? w.s.first + i : -1;
+        const int shift = w.few - w.low;  // place in the list of visible positions = position + shift, behind the first ones
+        const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
+        const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
+        const int v_few = a.mask.window > 0 ? (a.mask.sinks <= w.low ? w.few : min(a.mask.sinks, 1 << 30) + shift) : 0;
+        // places that every row of the tile sees: [0, few) and [lo_all, hi_all]
+        const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
+        const int hi_all = w.s.first + rr0 / a.rep + shift;
+        const int lo_all = a.mask.window > 0 ? w.s.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
+        const float scale = fabsf(a.scale);
+        float m = -INFINITY, l = 0.0f;
+        bool ok = true;
+        for (int j = 0; ok && j < w.tiles[x]; ++j) {
+            ok = mbar_wait(&bar.s_full[x], j & 1, &gave_up);
+            if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+            tc_fence_after();
+            float s[kPrPos];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, s_at + 32 * c);
+            tmem_wait_ld();
+            if (a.scale < 0.0f) {  // the largest of s times a negative scale is that of the smallest s
+#pragma unroll
+                for (int c = 0; c < kPrPos; ++c) s[c] = -s[c];
+            }
+            const int v0 = j * kPrPos;
+            const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 3]);
+            const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
+            const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= w.few);
+            if (!all) {
+                const uint32_t word[4] = {okw.x, okw.y, okw.z, okw.w};
+#pragma unroll
+                for (int c = 0; c < kPrPos; ++c) {
+                    const int v = v0 + c;
+                    const bool see = v <= v_hi && (v >= v_lo || v < v_few) && ((word[c >> 5] >> (c & 31)) & 1u);
+                    if (!see) s[c] = -INFINITY;
+                }
+            }
+            float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+            for (int c = 4; c < kPrPos; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+            const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
+            if (__any_sync(0xFFFFFFFFu, grow)) {
+                const float f = grow ? fast_exp2(m - top) : 1.0f;  // 0 where nothing was seen before
+                if (grow) m = top;
+                l *= f;
+                if (j > 0) {
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        float o[32];
+                        tmem_ld32(o, o_at + 32 * c);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] *= f;
+                        tmem_st32(o_at + 32 * c, o);
+                    }
+                }
+            }
+            const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t p[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p0 = fast_exp2(fmaf(s[32 * c + 2 * e], scale, -ref));
+                    const float p1 = fast_exp2(fmaf(s[32 * c + 2 * e + 1], scale, -ref));
+                    sum[c] += p0 + p1;
+                    p[e] = pack2_bits<CT>(p0, p1);
+                }
+                tmem_st16(s_at + 16 * c, p);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p_full[x]);
+        }
+        if (ok && w.tiles[x] > 0) {
+            ok = mbar_wait(&bar.o_full[x], 0, &gave_up);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            tc_fence_after();
+        }
+        if (ok) {
+            const int64_t at = static_cast<int64_t>(w.s.row0 + i) * a.heads + h;
+            float o[D];
+            if (w.tiles[x] > 0) {
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) tmem_ld32(o + 32 * c, o_at + 32 * c);
+                tmem_wait_ld();
+            } else {
+#pragma unroll
+                for (int c = 0; c < D; ++c) o[c] = 0.0f;
+            }
+            const bool none = l == 0.0f;
+            const float inv = 1.0f / l;
+            bool fin = true;
+#pragma unroll
+            for (int c = 0; c < D; ++c) {
+                fin &= fabsf(o[c]) <= 3.402823466e38f;
+                o[c] = none ? 0.0f : o[c] * inv;
+            }
+            if (live && fin) {
+                uint4* dst = reinterpret_cast<uint4*>(a.out + at * D);
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    const float* t = o + 8 * c;
+                    dst[c] = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
+                                                                pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
+                                                   : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
+                                                                pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
+                }
+                if (a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
+            }
+            // Rows whose sums are not finite: what they do not see may have been NaN or infinite (a weight of zero times it).
+            // Again, over what the row sees alone, on the fp32 pipe.
+            uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin);
+            for (; left != 0; left &= left - 1) {
+                const int who = __ffs(left) - 1;
+                const int wi = __shfl_sync(0xFFFFFFFFu, i, who), wh = __shfl_sync(0xFFFFFFFFu, h, who);
+                const int wp = __shfl_sync(0xFFFFFFFFu, pos, who);
+                constexpr int E = D / 32;
+                RowState<D> st;
+                float q[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    st.acc[e] = 0.0f;
+                    q[e] = a.scale * typed_value(a.q, a.q_type, (w.s.row0 + wi) * a.ldq + static_cast<int64_t>(wh) * D + lane * E + e);
+                }
+                if (wp >= 0) {
+                    const int low = paged_low(a.mask, wp);
+                    attend_row<D, CT>(a.w, w.b, w.kv_head, q, 0, paged_few(a.mask, low), st);
+                    attend_row<D, CT>(a.w, w.b, w.kv_head, q, low, wp + 1, st);
+                }
+                const int64_t wat = static_cast<int64_t>(w.s.row0 + wi) * a.heads + wh;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    a.out[wat * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
+                if (a.lse != nullptr && lane == 0) a.lse[wat] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
+            }
+        } else if (lane == 0) {
+            report_status(a.w.status, AFX_ERR_TIMEOUT);
+        }
+    }
+    // ---- nothing is in flight any more: all products were waited for by the rows' threads, all copies by the loaders
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 8) tmem_free(tmem, 512);
+}
+
+}  // namespace afx
