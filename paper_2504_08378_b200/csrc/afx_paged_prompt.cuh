@@ -32,15 +32,15 @@ afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, cudaStr
 
 template <int D>
 struct PrCfg {
-    static constexpr int kStages = D == 128 ? 2 : 3;
+    static constexpr int kRing = D == 128 ? 5 : 8;     // tiles of K and V on their way or in use, in the order of their use: K0, V0, K1, V1, ..
     static constexpr int kBlock = kPrPos * 128;        // bytes of 128 rows of 64 values
     static constexpr int kTile = kBlock * (D / 64);    // bytes of 128 rows of D values
-    static constexpr int kQ = 0, kK = kPrTiles * kTile, kV = kK + kStages * kTile;
-    static constexpr int kDyn = kV + kStages * kTile + 1024;  // (base rounded up to 1024)
+    static constexpr int kQ = 0, kKV = kPrTiles * kTile;
+    static constexpr int kDyn = kKV + kRing * kTile + 1024;  // (base rounded up to 1024)
 };
 
 struct PrBarriers {
-    uint64_t q_full, k_full[3], k_empty[3], v_full[3], v_empty[3], s_full[2], p_full[2], o_full[2], drain;
+    uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_full[2], drain;
 };
 
 // What a block works on.
@@ -58,7 +58,7 @@ __device__ __forceinline__ int pr_row_tiles(const PagedAttnArgs& a, const SeqSpa
 template <int D, int CT>
 __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnArgs a) {
     using Cfg = PrCfg<D>;
-    constexpr int ST = Cfg::kStages;
+    constexpr int NB = Cfg::kRing;
     constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
     extern __shared__ unsigned char dyn_raw[];
     __shared__ PrBarriers bar;
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
     __shared__ int gave_up;
     __shared__ PrWork work;
     __shared__ int warp_tiles[kPrThreads / 32];
-    __shared__ __align__(16) uint16_t page_ok[4][8];  // per tile of positions (mod 4) and 16 of them: the cache has them
+    __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const uint32_t base = smem_u32(dyn);
@@ -120,12 +120,10 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
     }
     if (tid == 0) {
         gave_up = 0;
-        mbar_init(&bar.q_full, kPrLoaders);
-        for (int i = 0; i < ST; ++i) {
-            mbar_init(&bar.k_full[i], kPrLoaders);
-            mbar_init(&bar.v_full[i], kPrLoaders);
-            mbar_init(&bar.k_empty[i], 1);
-            mbar_init(&bar.v_empty[i], 1);
+        mbar_init(&bar.q_full, kPrLoaders * 32);
+        for (int i = 0; i < NB; ++i) {
+            mbar_init(&bar.full[i], kPrLoaders * 32);
+            mbar_init(&bar.empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.s_full[i], 1);
@@ -153,9 +151,16 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
             if (lane == 0 && n_tiles > 0) {
                 constexpr uint32_t s_desc = mma_desc(CT == AFX_BF16, 128, kPrPos, false);
                 constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
-                bool ok = mbar_wait(&bar.q_full, 0, &gave_up);
+                // Tile n of the ring (2 j: K of positions j, 2 j + 1: V).  The loaders' copies are writes like any thread's, the
+                // products read shared memory by another path: the fence stands between what the barrier says and them.
+                auto arrived = [&](int n) {
+                    const bool in = mbar_wait(&bar.full[n % NB], (n / NB) & 1, &gave_up);
+                    fence_proxy_async();
+                    return in;
+                };
+                auto at = [&](int n) { return base + Cfg::kKV + (n % NB) * Cfg::kTile; };
                 auto scores = [&](int x, int j) {
-                    const uint32_t q = base + Cfg::kQ + x * Cfg::kTile, k = base + Cfg::kK + (j % ST) * Cfg::kTile;
+                    const uint32_t q = base + Cfg::kQ + x * Cfg::kTile, k = at(2 * j);
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
                         const uint32_t off = (i / 4) * Cfg::kBlock + (i % 4) * 32;
@@ -163,22 +168,21 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                     }
                     tc_commit(&bar.s_full[x]);
                 };
-                ok = ok && mbar_wait(&bar.k_full[0], 0, &gave_up);
-                tc_fence_after();
+                bool ok = mbar_wait(&bar.q_full, 0, &gave_up) && arrived(0);
                 if (ok) {
                     for (int x = 0; x < 2; ++x)
                         if (w.tiles[x] > 0) scores(x, 0);
-                    tc_commit(&bar.k_empty[0]);
+                    tc_commit(&bar.empty[0]);
                 }
                 for (int j = 0; ok && j < n_tiles; ++j) {
-                    ok = mbar_wait(&bar.v_full[j % ST], (j / ST) & 1, &gave_up);
-                    if (ok && j + 1 < n_tiles) ok = mbar_wait(&bar.k_full[(j + 1) % ST], ((j + 1) / ST) & 1, &gave_up);
+                    ok = arrived(2 * j + 1);
+                    if (ok && j + 1 < n_tiles) ok = arrived(2 * j + 2);
                     for (int x = 0; ok && x < 2; ++x) {
                         if (j >= w.tiles[x]) continue;
                         ok = mbar_wait(&bar.p_full[x], j & 1, &gave_up);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t v = base + Cfg::kV + (j % ST) * Cfg::kTile;
+                        const uint32_t v = at(2 * j + 1);
 #pragma unroll
                         for (int i = 0; i < kPrPos / 16; ++i)
                             tc_mma_ts(tmem + 256 + x * D, tmem + x * kPrPos + i * 8, smem_desc(v + i * 2048, Cfg::kBlock), o_desc, j > 0 || i > 0);
@@ -188,8 +192,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                             tc_commit(&bar.o_full[x]);
                     }
                     if (ok) {
-                        tc_commit(&bar.v_empty[j % ST]);
-                        if (j + 1 < n_tiles) tc_commit(&bar.k_empty[(j + 1) % ST]);
+                        tc_commit(&bar.empty[(2 * j + 1) % NB]);
+                        if (j + 1 < n_tiles) tc_commit(&bar.empty[(2 * j + 2) % NB]);
                     }
                 }
                 if (!ok) {  // what has been issued ends before tensor memory is given back
@@ -208,10 +212,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 const uint32_t at = tile + (piece >> 3) * Cfg::kBlock + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(src), "r"(bytes) : "memory");
             };
-            auto done = [&](uint64_t* full) {  // (after the wait for the copies)
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(full);
+            auto when_landed = [&](uint64_t* full) {  // an arrival of this thread's as soon as its copies so far have landed
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
             };
             for (int r0 = lw * RPI; r0 < kPrTiles * kPrRows; r0 += kPrLoaders * RPI) {
                 const int r = r0 + lane / PIECES, rr = w.row_base + r, piece = lane % PIECES;
@@ -220,7 +222,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 const int64_t at = live ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D + piece * 8 : 0;
                 put(base + Cfg::kQ + (r / kPrRows) * Cfg::kTile, r % kPrRows, piece, reinterpret_cast<const uint16_t*>(a.q) + at, live ? 16 : 0);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            when_landed(&bar.q_full);
             const int nv = max(w.tiles[0], w.tiles[1]) * kPrPos;  // (rows behind the last visible position are left out below)
             const int end = min(w.s.len, w.s.first + w.s.n);
             int64_t off[3], next[3];
@@ -236,7 +238,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                     }
                 }
             };
-            auto fill = [&](const uint16_t* pages, uint32_t tile) {
+            auto fill = [&](const uint16_t* pages, int n) {
+                const uint32_t tile = base + Cfg::kKV + (n % NB) * Cfg::kTile;
 #pragma unroll
                 for (int x = 0; x < 3; ++x) {
                     const int blk = lw + x * kPrLoaders;
@@ -248,42 +251,31 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                         put(tile, blk * 16 + row, piece, pages + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
+                when_landed(&bar.full[n % NB]);
+            };
+            auto room = [&](int n) {  // tile n - NB of the ring has been used
+                return n < NB || __all_sync(0xFFFFFFFFu, mbar_wait(&bar.empty[n % NB], ((n / NB) & 1) ^ 1, &gave_up));
             };
             bool ok = true;
             look_up(0);
-            // loads in the order Q, K0, V0, K1, V1, ..; three of them on their way, each reported when it has landed
-            for (int j = 0; ok && j < n_tiles; ++j) {
-                const int st = j % ST;
-                const uint32_t free_parity = ((j / ST) & 1) ^ 1;
+            for (int j = 0; j < n_tiles; ++j) {
 #pragma unroll
                 for (int x = 0; x < 3; ++x) off[x] = next[x];
                 if (j + 1 < n_tiles) look_up(j + 1);
-                if (j >= ST) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.k_empty[st], free_parity, &gave_up));
+                ok = room(2 * j);
                 if (!ok) break;
 #pragma unroll
                 for (int x = 0; x < 3; ++x) {
                     const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
-                    if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 3][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                    if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 7][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
                 }
-                fill(a.w.k, base + Cfg::kK + st * Cfg::kTile);
-                if (j > 0) {
-                    asm volatile("cp.async.wait_group 2;" ::: "memory");
-                    done(&bar.k_full[(j - 1) % ST]);
-                }
-                if (j >= ST) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.v_empty[st], free_parity, &gave_up));
+                fill(a.w.k, 2 * j);
+                ok = room(2 * j + 1);
                 if (!ok) break;
-                fill(a.w.v, base + Cfg::kV + st * Cfg::kTile);
-                asm volatile("cp.async.wait_group 2;" ::: "memory");
-                done(j == 0 ? &bar.q_full : &bar.v_full[(j - 1) % ST]);
+                fill(a.w.v, 2 * j + 1);
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (ok && n_tiles > 0) {
-                done(&bar.k_full[(n_tiles - 1) % ST]);
-                done(&bar.v_full[(n_tiles - 1) % ST]);
-            } else if (!ok && lane == 0) {
-                report_status(a.w.status, AFX_ERR_TIMEOUT);
-            }
+            if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -318,7 +310,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 for (int c = 0; c < kPrPos; ++c) s[c] = -s[c];
             }
             const int v0 = j * kPrPos;
-            const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 3]);
+            const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 7]);
             const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
             const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= w.few);
             if (!all) {
