@@ -40,7 +40,7 @@ struct PrCfg {
 };
 
 struct PrBarriers {
-    uint64_t q_full, full[8], empty[8], s_full[2], p_full[2], o_full[2], drain;
+    uint64_t q_full, full[8], empty[8], s_full[2], p_half[2], p_full[2], o_full[2], drain;
 };
 
 // What a block works on.
@@ -53,6 +53,14 @@ struct PrWork {
 
 __device__ __forceinline__ int pr_row_tiles(const PagedAttnArgs& a, const SeqSpan& s) {
     return static_cast<int>((static_cast<int64_t>(s.n) * a.rep + kPrTiles * kPrRows - 1) / (kPrTiles * kPrRows));
+}
+
+// Bits 0 .. n - 1 of a word (n <= 0: none, n >= 32: all).
+__device__ __forceinline__ uint32_t pr_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 template <int D, int CT>
@@ -127,6 +135,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.s_full[i], 1);
+            mbar_init(&bar.p_half[i], 4);
             mbar_init(&bar.p_full[i], 4);
             mbar_init(&bar.o_full[i], 1);
         }
@@ -179,13 +188,17 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                     if (ok && j + 1 < n_tiles) ok = arrived(2 * j + 2);
                     for (int x = 0; ok && x < 2; ++x) {
                         if (j >= w.tiles[x]) continue;
-                        ok = mbar_wait(&bar.p_full[x], j & 1, &gave_up);
-                        if (!ok) break;
-                        tc_fence_after();
                         const uint32_t v = at(2 * j + 1);
 #pragma unroll
-                        for (int i = 0; i < kPrPos / 16; ++i)
-                            tc_mma_ts(tmem + 256 + x * D, tmem + x * kPrPos + i * 8, smem_desc(v + i * 2048, Cfg::kBlock), o_desc, j > 0 || i > 0);
+                        for (int half = 0; half < 2; ++half) {
+                            ok = ok && mbar_wait(half == 0 ? &bar.p_half[x] : &bar.p_full[x], j & 1, &gave_up);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int i = half * (kPrPos / 32); i < (half + 1) * (kPrPos / 32); ++i)
+                                tc_mma_ts(tmem + 256 + x * D, tmem + x * kPrPos + i * 8, smem_desc(v + i * 2048, Cfg::kBlock), o_desc, j > 0 || i > 0);
+                        }
+                        if (!ok) break;
                         if (j + 1 < w.tiles[x])
                             scores(x, j + 1);
                         else
@@ -313,18 +326,23 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
             const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 7]);
             const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
             const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= w.few);
-            if (!all) {
+            if (!all) {  // 32 places as bits: those up to v_hi that are from v_lo on or below v_few, and have a page
                 const uint32_t word[4] = {okw.x, okw.y, okw.z, okw.w};
 #pragma unroll
-                for (int c = 0; c < kPrPos; ++c) {
-                    const int v = v0 + c;
-                    const bool see = v <= v_hi && (v >= v_lo || v < v_few) && ((word[c >> 5] >> (c & 31)) & 1u);
-                    if (!see) s[c] = -INFINITY;
+                for (int c = 0; c < 4; ++c) {
+                    const int v = v0 + 32 * c;
+                    const uint32_t see = pr_below(v_hi + 1 - v) & (~pr_below(v_lo - v) | pr_below(v_few - v)) & word[c];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) s[32 * c + e] = (see & (1u << e)) != 0u ? s[32 * c + e] : -INFINITY;
                 }
             }
             float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-            for (int c = 4; c < kPrPos; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
+            for (int c = 4; c + 7 < kPrPos; c += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], s[c + e], s[c + 4 + e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[kPrPos - 4 + e]);
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
             const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
             if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -344,20 +362,34 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 }
             }
             const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const f32x2 scale2 = pack_f32x2(scale, scale), ref2 = pack_f32x2(-ref, -ref), one2 = pack_f32x2(1.0f, 1.0f);
+            f32x2 sum[2] = {0, 0};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t p[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const float p0 = fast_exp2(fmaf(s[32 * c + 2 * e], scale, -ref));
-                    const float p1 = fast_exp2(fmaf(s[32 * c + 2 * e + 1], scale, -ref));
-                    sum[c] += p0 + p1;
+                    f32x2 t = ref2;
+                    fma_f32x2(t, pack_f32x2(s[32 * c + 2 * e], s[32 * c + 2 * e + 1]), scale2);
+                    float p0, p1;
+                    unpack_f32x2(t, p0, p1);
+                    p0 = fast_exp2(p0);
+                    p1 = fast_exp2(p1);
+                    fma_f32x2(sum[e & 1], pack_f32x2(p0, p1), one2);
                     p[e] = pack2_bits<CT>(p0, p1);
                 }
                 tmem_st16(s_at + 16 * c, p);
+                if (c == 1) {  // the first half of the positions may be multiplied
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bar.p_half[x]);
+                }
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            float sums[4];
+            unpack_f32x2(sum[0], sums[0], sums[1]);
+            unpack_f32x2(sum[1], sums[2], sums[3]);
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
