@@ -154,62 +154,95 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
     const int rows = w.s.n * a.rep;
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 8) {
-            // ---- products: one thread
-            if (lane == 0 && n_tiles > 0) {
+            // ---- products: the warp goes through the waits together and one lane issues, so that the operands'
+            // places stay in uniform registers (all of it in a lane's branch: 64 products took 3800 cycles of the thread's time)
+            if (n_tiles > 0) {
                 constexpr uint32_t s_desc = mma_desc(CT == AFX_BF16, 128, kPrPos, false);
                 constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
-                // Tile n of the ring (2 j: K of positions j, 2 j + 1: V).  The loaders' copies are writes like any thread's, the
+                const bool lead = elect_one();
+                const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+                const int nt = __shfl_sync(0xFFFFFFFFu, n_tiles, 0);
+                const int tiles[2] = {__shfl_sync(0xFFFFFFFFu, w.tiles[0], 0), __shfl_sync(0xFFFFFFFFu, w.tiles[1], 0)};
+                auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
+                // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies are writes like any thread's, the
                 // products read shared memory by another path: the fence stands between what the barrier says and them.
-                auto arrived = [&](int n) {
-                    const bool in = mbar_wait(&bar.full[n % NB], (n / NB) & 1, &gave_up);
+                int slot = 0;
+                uint32_t turn = 0;
+                auto arrived = [&]() {
+                    const bool in = wait(&bar.full[slot], turn);
                     fence_proxy_async();
                     return in;
                 };
-                auto at = [&](int n) { return base + Cfg::kKV + (n % NB) * Cfg::kTile; };
-                auto scores = [&](int x, int j) {
-                    const uint32_t q = base + Cfg::kQ + x * Cfg::kTile, k = at(2 * j);
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = (i / 4) * Cfg::kBlock + (i % 4) * 32;
-                        tc_mma_ss(tmem + x * kPrPos, smem_desc(q + off, 16), smem_desc(k + off, 16), s_desc, i > 0);
+                auto step = [&]() {
+                    if (++slot == NB) {
+                        slot = 0;
+                        turn ^= 1u;
                     }
-                    tc_commit(&bar.s_full[x]);
                 };
-                bool ok = mbar_wait(&bar.q_full, 0, &gave_up) && arrived(0);
+                auto scores = [&](int x, uint32_t k) {
+                    if (lead) {
+                        const uint32_t qd = smem_desc(base + Cfg::kQ + x * Cfg::kTile, 16), kd = smem_desc(base + Cfg::kKV + k * Cfg::kTile, 16);
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            const uint32_t off = ((i / 4) * Cfg::kBlock + (i % 4) * 32) >> 4;
+                            tc_mma_ss(tm + x * kPrPos, qd + off, kd + off, s_desc, i > 0);
+                        }
+                        tc_commit(&bar.s_full[x]);
+                    }
+                    __syncwarp();
+                };
+                bool ok = wait(&bar.q_full, 0) && arrived();
                 if (ok) {
+#pragma unroll
                     for (int x = 0; x < 2; ++x)
-                        if (w.tiles[x] > 0) scores(x, 0);
-                    tc_commit(&bar.empty[0]);
+                        if (tiles[x] > 0) scores(x, 0);
+                    if (lead) tc_commit(&bar.empty[0]);
+                    __syncwarp();
+                    step();
                 }
-                for (int j = 0; ok && j < n_tiles; ++j) {
-                    ok = arrived(2 * j + 1);
-                    if (ok && j + 1 < n_tiles) ok = arrived(2 * j + 2);
-                    for (int x = 0; ok && x < 2; ++x) {
-                        if (j >= w.tiles[x]) continue;
-                        const uint32_t v = at(2 * j + 1);
+                for (int j = 0; ok && j < nt; ++j) {
+                    ok = arrived();
+                    if (!ok) break;
+                    const int vs = slot;
+                    step();
+                    const int ks = slot;
+                    if (j + 1 < nt) {
+                        ok = arrived();
+                        step();
+                        if (!ok) break;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (!ok || j >= tiles[x]) continue;
+                        const uint32_t vd = smem_desc(base + Cfg::kKV + vs * Cfg::kTile, Cfg::kBlock);
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            ok = ok && mbar_wait(half == 0 ? &bar.p_half[x] : &bar.p_full[x], j & 1, &gave_up);
-                            if (!ok) break;
+                            ok = ok && wait(half == 0 ? &bar.p_half[x] : &bar.p_full[x], j & 1);
                             tc_fence_after();
+                            if (ok && lead) {
 #pragma unroll
-                            for (int i = half * (kPrPos / 32); i < (half + 1) * (kPrPos / 32); ++i)
-                                tc_mma_ts(tmem + 256 + x * D, tmem + x * kPrPos + i * 8, smem_desc(v + i * 2048, Cfg::kBlock), o_desc, j > 0 || i > 0);
+                                for (int i = half * (kPrPos / 32); i < (half + 1) * (kPrPos / 32); ++i)
+                                    tc_mma_ts(tm + 256 + x * D, tm + x * kPrPos + i * 8, vd + i * (2048 >> 4), o_desc, j > 0 || i > 0);
+                            }
+                            __syncwarp();
                         }
-                        if (!ok) break;
-                        if (j + 1 < w.tiles[x])
-                            scores(x, j + 1);
-                        else
-                            tc_commit(&bar.o_full[x]);
+                        if (!ok) continue;
+                        if (j + 1 < tiles[x]) {
+                            scores(x, ks);
+                        } else {
+                            if (lead) tc_commit(&bar.o_full[x]);
+                            __syncwarp();
+                        }
                     }
-                    if (ok) {
-                        tc_commit(&bar.empty[(2 * j + 1) % NB]);
-                        if (j + 1 < n_tiles) tc_commit(&bar.empty[(2 * j + 2) % NB]);
+                    if (ok && lead) {
+                        tc_commit(&bar.empty[vs]);
+                        if (j + 1 < nt) tc_commit(&bar.empty[ks]);
                     }
+                    __syncwarp();
                 }
-                if (!ok) {  // what has been issued ends before tensor memory is given back
+                if (!ok && lead) {  // what has been issued ends before tensor memory is given back
                     int alone = 0;
                     report_status(a.w.status, AFX_ERR_TIMEOUT);
                     tc_commit(&bar.drain);
@@ -291,7 +324,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
             if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---- softmax: a thread per row
         const int x = warp >> 2, r = (warp & 3) * 32 + lane, rr = w.row_base + x * kPrRows + r;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;

@@ -95,42 +95,55 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r) {
 // ---- products
 
 // Operand in shared memory with the 128-byte swizzle (16-byte piece c of row r at piece c ^ (r & 7) of its 128 bytes, groups
-// of 8 rows 1024 bytes apart, base on 1024 bytes).  lead: bytes from one 128-byte-wide block to the next, where the
-// operand's contiguous axis is not the one that is summed over (ignored otherwise).
-__device__ __forceinline__ uint64_t smem_desc(uint32_t at, uint32_t lead) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((at & 0x3FFFFu) >> 4);
-    d |= static_cast<uint64_t>(lead >> 4) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;  // descriptor version of sm_100
-    d |= static_cast<uint64_t>(2) << 61;  // 128-byte swizzle
-    return d;
-}
+// of 8 rows 1024 bytes apart, base on 1024 bytes): the low word of its descriptor, which holds the place, and the high one.
+// lead: bytes from one 128-byte-wide block to the next, where the operand's contiguous axis is not the one that is
+// summed over (ignored otherwise).  A place x bytes further on is x / 16 more in the low word.
+__device__ __forceinline__ uint32_t smem_desc(uint32_t at, uint32_t lead) { return ((at & 0x3FFFFu) >> 4) | ((lead >> 4) << 16); }
+constexpr uint32_t kSmemDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);  // group stride, version of sm_100, 128-byte swizzle
+
 // fp32 accumulator, 16-bit operands of one type, A with the summed axis contiguous; b_mn: B's other axis is contiguous.
 __device__ __forceinline__ constexpr uint32_t mma_desc(bool bf16, int m, int n, bool b_mn) {
     return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
            (static_cast<uint32_t>(m >> 4) << 24);
 }
-// D[tmem] (+)= A[smem] B[smem], 16 of the summed axis
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t is;
     asm volatile(
         "{\n"
         ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        "elect.sync _|p, 0xFFFFFFFF;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(is));
+    return is != 0;
+}
+// D[tmem] (+)= A[smem] B[smem], 16 of the summed axis.  (The operands' places are values that all lanes of the warp
+// share: the instruction takes them from uniform registers.)
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b64 x, y;\n"
+        "setp.ne.b32 p, %5, 0;\n"
+        "mov.b64 x, {%1, %4};\n"
+        "mov.b64 y, {%2, %4};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n"
         "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add))
+        "r"(a), "r"(b), "r"(idesc), "r"(kSmemDescHigh), "r"(static_cast<uint32_t>(add))
         : "memory");
 }
 // D[tmem] (+)= A[tmem] B[smem]
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add) {
     asm volatile(
         "{\n"
         ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        ".reg .b64 y;\n"
+        "setp.ne.b32 p, %5, 0;\n"
+        "mov.b64 y, {%2, %4};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n"
         "}\n" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add))
+        "r"(a), "r"(b), "r"(idesc), "r"(kSmemDescHigh), "r"(static_cast<uint32_t>(add))
         : "memory");
 }
 // The barrier gets an arrival when every product issued by this thread so far is done.
