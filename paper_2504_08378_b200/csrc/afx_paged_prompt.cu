@@ -4,6 +4,38 @@
 
 namespace afx {
 
+typedef CUresult (*TensorMapEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                    const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                    CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static TensorMapEncode tensor_map_encode() {
+    static const TensorMapEncode fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<TensorMapEncode>(p);
+    }();
+    return fn;
+}
+
+// The pool as a tensor [page][kv head][position in the page][dim], read in boxes of `box` positions and 64 dims.
+static bool pool_map(CUtensorMap* map, void* pages, int dtype, int D, const PagedView& w, int box) {
+    const TensorMapEncode encode = tensor_map_encode();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(w.page_size), static_cast<cuuint64_t>(w.n_kv),
+                                static_cast<cuuint64_t>(w.n_pages)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(w.pos_stride) * 2, static_cast<cuuint64_t>(w.head_stride) * 2,
+                                   static_cast<cuuint64_t>(w.page_stride) * 2};
+    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box), 1, 1}, steps[4] = {1, 1, 1, 1};
+    return encode(map, dtype == AFX_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pages, dims, strides, boxes,
+                  steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, int CT>
 static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     const auto kern = paged_prompt_kernel<D, CT>;
@@ -15,6 +47,12 @@ static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     // sums of rows rounded up to pairs of row tiles, at most
     const int64_t pairs = static_cast<int64_t>(a.w.n_tokens) * a.rep / (kPrTiles * kPrRows) + a.w.n_seqs;
     if (pairs * a.w.n_kv > 0x7FFFFFFF) return AFX_ERR_CAPACITY;
+    PagedPromptArgs args = {a, 1};
+    CUtensorMap maps[2] = {};
+    int box = 1;
+    while (box < kPrPos && a.w.page_size % (2 * box) == 0) box *= 2;
+    // (what the encoder refuses -- strides of 2^40 bytes, no such entry point -- is read row by row)
+    if (box >= 16 && pool_map(&maps[0], a.w.k, CT, D, a.w, box) && pool_map(&maps[1], a.w.v, CT, D, a.w, box)) args.box = box;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -25,7 +63,7 @@ static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kern, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kern, args, maps[0], maps[1]) != cudaSuccess) {
         cudaGetLastError();
         return AFX_ERR_CUDA;
     }

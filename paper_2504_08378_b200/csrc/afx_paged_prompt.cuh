@@ -12,7 +12,10 @@
 // below 2^8; fp16 P is carried times 2^7, so that what is lost below its range is 2^-32 of the largest weight).
 // P is rounded to the cache's type (half a step of 2^-9 / 2^-12 relative per weight, averaged over the weights; the sums
 // of weights are taken before that rounding): 16-bit operands are what the tensor cores multiply at full rate.
-// Three warps fetch keys and values with cp.async, rows by way of the page table, any page size.
+// Three warps fetch keys and values.  Pages of a multiple of 16 positions are read in boxes of 16 to 128 positions (the
+// largest power of two that divides the page size) with tensor copies; other pages, and the tile in which the sequence
+// ends (what lies behind it in its page may be anything, and has to become zero), row by row with cp.async.  (Everything with
+// cp.async: the tensor cores waited 1300 of 4000 cycles per step for the copies.)
 //
 // Bound by the exponentials and the products alike: 2 x 128 x 128 exponentials are 2048 cycles of an SM's 16 per cycle, the four products
 // 2048 cycles at D = 128.
@@ -27,6 +30,11 @@ constexpr int kPrThreads = 384;  // warps 0-3: rows of tile 0, 4-7: tile 1, 8: p
 constexpr int kPrRows = 128, kPrTiles = 2, kPrPos = 128;
 constexpr int kPrLoaders = 3;
 constexpr float kPrGrow = 8.0f;  // powers of two that a row's maximum may grow by before O is rescaled
+
+struct PagedPromptArgs {
+    PagedAttnArgs a;
+    int box;  // positions of a tensor copy; 1: none are made
+};
 
 afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, cudaStream_t st);  // afx_paged_prompt.cu
 
@@ -64,7 +72,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 template <int D, int CT>
-__global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kPrThreads, 1)
+paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    const PagedAttnArgs& a = args.a;
     using Cfg = PrCfg<D>;
     constexpr int NB = Cfg::kRing;
     constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
@@ -112,8 +122,9 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                     w.row_base = (t - 1 - (pair - before)) * kPrTiles * kPrRows;
                     const int rows = s.n * a.rep;
                     const int first = max(s.first + w.row_base / a.rep, 0);
-                    w.low = paged_low(a.mask, first);
-                    w.few = paged_few(a.mask, w.low);
+                    // (both on a box's border; places that no row sees are masked)
+                    w.low = paged_low(a.mask, first) & ~(args.box - 1);
+                    w.few = min((paged_few(a.mask, w.low) + args.box - 1) & ~(args.box - 1), w.low);
                     for (int x = 0; x < kPrTiles; ++x) {
                         const int r0 = w.row_base + x * kPrRows, r1 = min(r0 + kPrRows, rows) - 1;
                         const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
@@ -269,7 +280,6 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 put(base + Cfg::kQ + (r / kPrRows) * Cfg::kTile, r % kPrRows, piece, reinterpret_cast<const uint16_t*>(a.q) + at, live ? 16 : 0);
             }
             when_landed(&bar.q_full);
-            const int nv = max(w.tiles[0], w.tiles[1]) * kPrPos;  // (rows behind the last visible position are left out below)
             const int end = min(w.s.len, w.s.first + w.s.n);
             int64_t off[3], next[3];
             auto look_up = [&](int j) {
@@ -278,11 +288,33 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                     const int v = j * kPrPos + (lw + x * kPrLoaders) * 16 + (lane & 15);
                     const int p = v < w.few ? v : v - w.few + w.low;
                     next[x] = -1;
-                    if (lw + x * kPrLoaders < 8 && v < nv && p < end) {
+                    if (lw + x * kPrLoaders < 8 && p < end) {
                         next[x] = paged_row(a.w, w.b, p, w.kv_head);
                         if (next[x] < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
                     }
                 }
+            };
+            // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).
+            const int boxes = kPrPos / args.box;
+            // first tile that is not: it holds the sequence's end or (box = 1) any
+            const int n_boxed = args.box == 1 ? 0 : w.few + end - w.low >= 0 ? (w.few + end - w.low) / kPrPos : 0;
+            int page = -1, in_page = 0;
+            auto look_up_box = [&](int j) {
+                const int v = j * kPrPos + (lane % boxes) * args.box, p = v < w.few ? v : v - w.few + w.low;
+                page = paged_page(a.w, w.b, p, in_page);
+                if (page < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
+            };
+            auto fill_boxes = [&](const CUtensorMap* map, int n) {
+                const uint32_t tile = base + Cfg::kKV + (n % NB) * Cfg::kTile;
+                if (lane == 0) mbar_expect(&bar.full[n % NB], Cfg::kTile);
+                __syncwarp();
+                for (int x = lane; x < boxes * (D / 64); x += 32) {  // (boxes divides 32 or x stays below 32: the lane's own box)
+                    const int half = x / boxes, i = x % boxes;
+                    // a page that is none: out of the tensor, zeros
+                    tma_load_4d(tile + half * Cfg::kBlock + i * args.box * 128, map, half * 64, in_page, w.kv_head, page < 0 ? a.w.n_pages : page,
+                                &bar.full[n % NB]);
+                }
+                if (lane != 0) mbar_arrive(&bar.full[n % NB]);
             };
             auto fill = [&](const uint16_t* pages, int n) {
                 const uint32_t tile = base + Cfg::kKV + (n % NB) * Cfg::kTile;
@@ -303,22 +335,41 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
                 return n < NB || __all_sync(0xFFFFFFFFu, mbar_wait(&bar.empty[n % NB], ((n / NB) & 1) ^ 1, &gave_up));
             };
             bool ok = true;
-            look_up(0);
+            if (lw < n_boxed) look_up_box(lw);
+            if (n_boxed == 0) look_up(0);
             for (int j = 0; j < n_tiles; ++j) {
+                const bool boxed = j < n_boxed, mine = boxed && j % kPrLoaders == lw;
+                if (!boxed) {
 #pragma unroll
-                for (int x = 0; x < 3; ++x) off[x] = next[x];
-                if (j + 1 < n_tiles) look_up(j + 1);
+                    for (int x = 0; x < 3; ++x) off[x] = next[x];
+                }
+                if (j + 1 < n_tiles && j + 1 >= n_boxed) look_up(j + 1);
                 ok = room(2 * j);
                 if (!ok) break;
+                if (!boxed) {
 #pragma unroll
-                for (int x = 0; x < 3; ++x) {
-                    const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
-                    if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 7][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                    for (int x = 0; x < 3; ++x) {
+                        const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
+                        if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 7][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                    }
+                    fill(a.w.k, 2 * j);
+                } else if (mine) {
+                    const uint32_t m = __ballot_sync(0xFFFFFFFFu, page >= 0);
+                    if (lane < 8) page_ok[j & 7][lane] = (m >> (lane * 16 / args.box)) & 1u ? 0xFFFFu : 0u;
+                    fill_boxes(&k_map, 2 * j);
+                } else {
+                    mbar_arrive(&bar.full[2 * j % NB]);
                 }
-                fill(a.w.k, 2 * j);
                 ok = room(2 * j + 1);
                 if (!ok) break;
-                fill(a.w.v, 2 * j + 1);
+                if (!boxed) {
+                    fill(a.w.v, 2 * j + 1);
+                } else if (mine) {
+                    fill_boxes(&v_map, 2 * j + 1);
+                    if (j + kPrLoaders < n_boxed) look_up_box(j + kPrLoaders);
+                } else {
+                    mbar_arrive(&bar.full[(2 * j + 1) % NB]);
+                }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
@@ -335,8 +386,8 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
         const int shift = w.few - w.low;  // place in the list of visible positions = position + shift, behind the first ones
         const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
         const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
-        const int v_few = a.mask.window > 0 ? (a.mask.sinks <= w.low ? w.few : min(a.mask.sinks, 1 << 30) + shift) : 0;
-        // places that every row of the tile sees: [0, few) and [lo_all, hi_all]
+        const int v_few = a.mask.window > 0 ? a.mask.sinks : 0;  // (first positions are their own places: few covers them, or few = low)
+        // places that every row of the tile sees: below v_few and [lo_all, hi_all]
         const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
         const int hi_all = w.s.first + rr0 / a.rep + shift;
         const int lo_all = a.mask.window > 0 ? w.s.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
@@ -358,7 +409,7 @@ __global__ void __launch_bounds__(kPrThreads, 1) paged_prompt_kernel(PagedAttnAr
             const int v0 = j * kPrPos;
             const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 7]);
             const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
-            const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= w.few);
+            const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= v_few);
             if (!all) {  // 32 places as bits: those up to v_hi that are from v_lo on or below v_few, and have a page
                 const uint32_t word[4] = {okw.x, okw.y, okw.z, okw.w};
 #pragma unroll
