@@ -49,8 +49,10 @@ static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     if (pairs * a.w.n_kv > 0x7FFFFFFF) return AFX_ERR_CAPACITY;
     PagedPromptArgs args = {a, 1};
     CUtensorMap maps[2] = {};
+    // (with a window the positions begin on a box's border, and the first ones end on one: small boxes leave less to mask)
+    const int most = a.mask.window > 0 ? 16 : kPrPos;
     int box = 1;
-    while (box < kPrPos && a.w.page_size % (2 * box) == 0) box *= 2;
+    while (box < most && a.w.page_size % (2 * box) == 0) box *= 2;
     // (what the encoder refuses -- strides of 2^40 bytes, no such entry point -- is read row by row)
     if (box >= 16 && pool_map(&maps[0], a.w.k, CT, D, a.w, box) && pool_map(&maps[1], a.w.v, CT, D, a.w, box)) args.box = box;
     cudaLaunchAttribute attr[1];

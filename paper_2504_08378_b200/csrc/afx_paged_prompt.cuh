@@ -71,6 +71,19 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+// Two weights 2^(s scale + ref), added to the sums, rounded and packed.
+template <int CT>
+__device__ __forceinline__ uint32_t pr_weights(float s0, float s1, f32x2 scale, f32x2 ref, f32x2& sum) {
+    float p0, p1;
+    f32x2 t = ref;
+    fma_f32x2(t, pack_f32x2(s0, s1), scale);
+    unpack_f32x2(t, p0, p1);
+    p0 = fast_exp2(p0);
+    p1 = fast_exp2(p1);
+    fma_f32x2(sum, pack_f32x2(p0, p1), pack_f32x2(1.0f, 1.0f));
+    return pack2_bits<CT>(p0, p1);
+}
+
 template <int D, int CT>
 __global__ void __launch_bounds__(kPrThreads, 1)
 paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -139,7 +152,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     }
     if (tid == 0) {
         gave_up = 0;
-        mbar_init(&bar.q_full, kPrLoaders * 32);
+        mbar_init(&bar.q_full, kPrTiles * kPrRows);
         for (int i = 0; i < NB; ++i) {
             mbar_init(&bar.full[i], kPrLoaders * 32);
             mbar_init(&bar.empty[i], 1);
@@ -272,14 +285,6 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             auto when_landed = [&](uint64_t* full) {  // an arrival of this thread's as soon as its copies so far have landed
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
             };
-            for (int r0 = lw * RPI; r0 < kPrTiles * kPrRows; r0 += kPrLoaders * RPI) {
-                const int r = r0 + lane / PIECES, rr = w.row_base + r, piece = lane % PIECES;
-                const int i = rr / a.rep;
-                const bool live = rr < rows;
-                const int64_t at = live ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D + piece * 8 : 0;
-                put(base + Cfg::kQ + (r / kPrRows) * Cfg::kTile, r % kPrRows, piece, reinterpret_cast<const uint16_t*>(a.q) + at, live ? 16 : 0);
-            }
-            when_landed(&bar.q_full);
             const int end = min(w.s.len, w.s.first + w.s.n);
             int64_t off[3], next[3];
             auto look_up = [&](int j) {
@@ -387,6 +392,21 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
         const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
         const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
         const int v_few = a.mask.window > 0 ? a.mask.sinks : 0;  // (first positions are their own places: few covers them, or few = low)
+        {  // the warp's 32 query rows into shared memory, 16 (or 8) lanes to a row
+            constexpr int PIECES = D / 8, RPI = 32 / PIECES;
+            const int64_t from = live ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(h) * D : -1;
+            const uint32_t tile = base + Cfg::kQ + x * Cfg::kTile;
+#pragma unroll
+            for (int k = 0; k < 32 / RPI; ++k) {
+                const int row = k * RPI + lane / PIECES, piece = lane % PIECES, tr = (warp & 3) * 32 + row;
+                const int64_t o = __shfl_sync(0xFFFFFFFFu, from, row);
+                const uint32_t to = tile + (piece >> 3) * Cfg::kBlock + tr * 128 + (((piece & 7) ^ (tr & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to),
+                             "l"(reinterpret_cast<const uint16_t*>(a.q) + (o < 0 ? 0 : o) + piece * 8), "r"(o < 0 ? 0 : 16)
+                             : "memory");
+            }
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar.q_full)) : "memory");
+        }
         // places that every row of the tile sees: below v_few and [lo_all, hi_all]
         const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
         const int hi_all = w.s.first + rr0 / a.rep + shift;
@@ -420,56 +440,61 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     for (int e = 0; e < 32; ++e) s[32 * c + e] = (see & (1u << e)) != 0u ? s[32 * c + e] : -INFINITY;
                 }
             }
-            float mx[4] = {s[0], s[1], s[2], s[3]};
+            if (j == 0) {  // the first maximum is the reference; afterwards it stays while it is not exceeded by far
+                float top = fmaxf(s[0], s[1]);
 #pragma unroll
-            for (int c = 4; c + 7 < kPrPos; c += 8)
+                for (int c = 2; c < kPrPos; c += 2) top = max3(top, s[c], s[c + 1]);
+                m = top * scale;
+            }
+            const f32x2 scale2 = pack_f32x2(scale, scale);
+            uint32_t p[kPrPos / 4];
+            f32x2 sum[2];
+            // The first half of the weights and, beside them, the maximum of all scores; when a row's has grown by too much
+            // (seldom), the rows' sums so far are rescaled and the weights taken again.
+            for (int pass = 0; pass < 2; ++pass) {
+                const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
+                const f32x2 ref2 = pack_f32x2(-ref, -ref);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                sum[0] = sum[1] = 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], s[c + e], s[c + 4 + e]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[kPrPos - 4 + e]);
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-            const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
-            if (__any_sync(0xFFFFFFFFu, grow)) {
+                for (int e = 0; e < kPrPos / 4; ++e) {
+                    p[e] = pr_weights<CT>(s[2 * e], s[2 * e + 1], scale2, ref2, sum[e & 1]);
+                    mx[(2 * e) & 3] = max3(mx[(2 * e) & 3], s[4 * e], s[4 * e + 1]);
+                    mx[(2 * e + 1) & 3] = max3(mx[(2 * e + 1) & 3], s[4 * e + 2], s[4 * e + 3]);
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
+                if (pass == 1 || !__any_sync(0xFFFFFFFFu, grow)) break;
                 const float f = grow ? fast_exp2(m - top) : 1.0f;  // 0 where nothing was seen before
                 if (grow) m = top;
                 l *= f;
-                if (j > 0) {
+                if (j > 0) {  // (the scores are there: what was issued before them, O's last addition too, is done)
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        float o[32];
-                        tmem_ld32(o, o_at + 32 * c);
+                    for (int c = 0; c < D / 16; ++c) {
+                        float o[16];
+                        tmem_ld16(o, o_at + 16 * c);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] *= f;
-                        tmem_st32(o_at + 32 * c, o);
+                        for (int e = 0; e < 16; ++e) o[e] *= f;
+                        tmem_st16(o_at + 16 * c, reinterpret_cast<const uint32_t*>(o));
                     }
                 }
             }
-            const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
-            const f32x2 scale2 = pack_f32x2(scale, scale), ref2 = pack_f32x2(-ref, -ref), one2 = pack_f32x2(1.0f, 1.0f);
-            f32x2 sum[2] = {0, 0};
+            tmem_st16(s_at, p);
+            tmem_st16(s_at + 16, p + 16);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.p_half[x]);  // half of the positions may be multiplied
+            {
+                const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
+                const f32x2 ref2 = pack_f32x2(-ref, -ref);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t p[16];
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    f32x2 t = ref2;
-                    fma_f32x2(t, pack_f32x2(s[32 * c + 2 * e], s[32 * c + 2 * e + 1]), scale2);
-                    float p0, p1;
-                    unpack_f32x2(t, p0, p1);
-                    p0 = fast_exp2(p0);
-                    p1 = fast_exp2(p1);
-                    fma_f32x2(sum[e & 1], pack_f32x2(p0, p1), one2);
-                    p[e] = pack2_bits<CT>(p0, p1);
-                }
-                tmem_st16(s_at + 16 * c, p);
-                if (c == 1) {  // the first half of the positions may be multiplied
-                    tmem_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bar.p_half[x]);
-                }
+                for (int e = 0; e < kPrPos / 4; ++e)
+                    p[e] = pr_weights<CT>(s[kPrPos / 2 + 2 * e], s[kPrPos / 2 + 2 * e + 1], scale2, ref2, sum[e & 1]);
             }
+            tmem_st16(s_at + 32, p);
+            tmem_st16(s_at + 48, p + 16);
             float sums[4];
             unpack_f32x2(sum[0], sums[0], sums[1]);
             unpack_f32x2(sum[1], sums[2], sums[3]);
@@ -479,6 +504,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.p_full[x]);
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         if (ok && w.tiles[x] > 0) {
             ok = mbar_wait(&bar.o_full[x], 0, &gave_up);
             ok = __all_sync(0xFFFFFFFFu, ok);
@@ -503,18 +529,36 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 fin &= fabsf(o[c]) <= 3.402823466e38f;
                 o[c] = none ? 0.0f : o[c] * inv;
             }
-            if (live && fin) {
-                uint4* dst = reinterpret_cast<uint4*>(a.out + at * D);
+            {  // through the shared memory of the warp's queries, so that rows leave in whole lines
+                constexpr int PIECES = D / 8, RPI = 32 / PIECES;
+                const uint32_t mine = base + Cfg::kQ + x * Cfg::kTile + (warp & 3) * 32 * D * 2;
+                __syncwarp();
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
+                for (int c = 0; c < PIECES; ++c) {
                     const float* t = o + 8 * c;
-                    dst[c] = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
-                                                                pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
-                                                   : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
-                                                                pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
+                    const uint4 y = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
+                                                                       pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
+                                                          : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
+                                                                       pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(mine + lane * (D * 2) + ((c ^ (lane & 7)) << 4)), "r"(y.x),
+                                 "r"(y.y), "r"(y.z), "r"(y.w)
+                                 : "memory");
                 }
-                if (a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
+                __syncwarp();
+                const uint32_t good = __ballot_sync(0xFFFFFFFFu, live && fin);
+#pragma unroll
+                for (int k = 0; k < 32 / RPI; ++k) {
+                    const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
+                    const int64_t to = __shfl_sync(0xFFFFFFFFu, at, row);
+                    uint4 y;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w)
+                                 : "r"(mine + row * (D * 2) + ((piece ^ (row & 7)) << 4))
+                                 : "memory");
+                    if ((good >> row) & 1u) reinterpret_cast<uint4*>(a.out + to * D)[piece] = y;
+                }
             }
+            if (live && fin && a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
             // Rows whose sums are not finite: what they do not see may have been NaN or infinite (a weight of zero times it).
             // Again, over what the row sees alone, on the fp32 pipe.
             uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin);
