@@ -47,6 +47,7 @@ static afx_status launch_few_dt(const PagedFewArgs& f, bool pack, cudaStream_t s
 afx_status launch_paged_few(int dtype, int D, PagedFewArgs& f, cudaStream_t st) {
     const bool pack = few_packed(f.a.w.max_new, f.a.rep);
     f.rows_per_group = pack ? 8 : kFewRows;
+    f.rep_mul = static_cast<uint32_t>((uint64_t{1} << 32) / f.a.rep) + 1u;
     if (D == 128) return dtype == AFX_F16 ? launch_few_dt<128, AFX_F16>(f, pack, st) : launch_few_dt<128, AFX_BF16>(f, pack, st);
     return dtype == AFX_F16 ? launch_few_dt<64, AFX_F16>(f, pack, st) : launch_few_dt<64, AFX_BF16>(f, pack, st);
 }

@@ -37,7 +37,7 @@ struct FewCfg {
 };
 
 // What an item costs beside its tiles (queries, the warps' sums), in tiles: the ranges are cut with it counted in.
-constexpr int kFewItemCost = 1;
+constexpr int kFewItemCost = 3;
 
 // The workspace: a descriptor per range, then slots of an unfinished item's sums (m[16], l[16], acc[16][D]).  Slot 2 i is
 // the piece that range i begins with where the item began in an earlier range, 2 i + 1 the piece of the item that begins in
@@ -57,6 +57,7 @@ __host__ __device__ constexpr size_t few_workspace_bytes(int D) {
 struct PagedFewArgs {
     PagedAttnArgs a;
     int rows_per_group;  // 8 (packed) or 16
+    uint32_t rep_mul;    // r / rep = (r * rep_mul) >> 32 for 0 <= r < 2^16 (rep > 1)
     FewJoin* joins;
     float* slots;
 };
@@ -70,6 +71,7 @@ struct FewSeq {
     int few, low, nv;  // visible positions: [0, few) and low ..; nv of them
     int tiles;         // per item
     int items;         // kv heads times row groups
+    int groups;        // row groups
 };
 
 __device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool report) {
@@ -79,14 +81,22 @@ __device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool rep
     q.low = paged_low(f.a.mask, first);
     q.few = paged_few(f.a.mask, q.low);
     q.nv = max(end - q.low, 0) + (end > q.low ? q.few : 0);
-    q.items = q.s.n > 0 ? f.a.w.n_kv * ((q.s.n * f.a.rep + f.rows_per_group - 1) / f.rows_per_group) : 0;
+    q.groups = (q.s.n * f.a.rep + f.rows_per_group - 1) >> (f.rows_per_group == 8 ? 3 : 4);
+    q.items = f.a.w.n_kv * q.groups;
     q.tiles = (q.nv + kFewTile - 1) / kFewTile;
     return q;
+}
+
+// a / b of non-negative numbers that usually have 32 bits (the 64-bit quotient is a hundred instructions)
+__device__ __forceinline__ int64_t few_quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
 }
 
 // Where a range begins in the list (units: tiles, and kFewItemCost in front of an item's).
 struct FewStart {
     int64_t before;  // units in front of the sequence
+    FewSeq q;
     int b;
 };
 struct FewScratch {
@@ -122,14 +132,15 @@ __device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* s
 __device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int64_t mine_before, int64_t mine) {
     if (at < mine_before || at >= mine_before + mine) return;
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads;
-    int b = threadIdx.x * per;
-    for (; b < min(n, static_cast<int>(threadIdx.x + 1) * per) - 1; ++b) {
+    for (int b = threadIdx.x * per; b < min(n, static_cast<int>(threadIdx.x + 1) * per); ++b) {
         const FewSeq q = few_seq(f, b, false);
         const int64_t t = static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
-        if (mine_before + t > at) break;
+        if (mine_before + t > at) {
+            sc->start = {mine_before, q, b};
+            break;
+        }
         mine_before += t;
     }
-    sc->start = {mine_before, b};
 }
 // Range i holds units [i per + min(i, rest), ..): the first `rest` ranges one more.
 struct FewRanges {
@@ -137,13 +148,13 @@ struct FewRanges {
     int rest, n;
     __device__ __forceinline__ FewRanges(int64_t total, int blocks) {
         n = static_cast<int>(min(static_cast<int64_t>(blocks), total));
-        per = n > 0 ? total / n : 0;
+        per = n > 0 ? few_quotient(total, n) : 0;
         rest = n > 0 ? static_cast<int>(total - per * n) : 0;
     }
     __device__ __forceinline__ int64_t begin(int i) const { return per * i + min(i, rest); }
     __device__ __forceinline__ int of(int64_t unit) const {
         const int64_t wide = (per + 1) * rest;
-        return static_cast<int>(unit < wide ? unit / (per + 1) : rest + (unit - wide) / per);
+        return static_cast<int>(unit < wide ? few_quotient(unit, per + 1) : rest + few_quotient(unit - wide, per));
     }
 };
 
@@ -151,6 +162,7 @@ struct FewRanges {
 struct FewWalk {
     FewSeq q;
     int b, item;
+    int kv_head, group;  // of the item
     int t0, t1;         // this piece's tiles of the item
     int64_t left;       // units of the range behind this piece
     bool more;          // there is a piece
@@ -161,6 +173,9 @@ struct FewWalk {
         left -= u1 - u0;
         t0 = max(u0 - kFewItemCost, 0);
         t1 = max(u1 - kFewItemCost, 0);
+        kv_head = item;
+        if (q.groups > 1) kv_head = static_cast<int>(static_cast<uint32_t>(item) / static_cast<uint32_t>(q.groups));
+        group = item - kv_head * q.groups;
         return t1 > t0 || q.tiles == 0;
     }
     __device__ __forceinline__ void next(const PagedFewArgs& f) {
@@ -220,13 +235,18 @@ __device__ __forceinline__ void few_split(float a, float b, uint32_t& hi, uint32
     lo = pack2_bits<CT>(a - f.x, b - f.y);
 }
 
+// Token of row rr of the sequence's rows.  rep_mul = floor(2^32 / rep) + 1 exceeds 2^32 / rep by at most 1: rr times that is below 1 / rep.
+__device__ __forceinline__ int few_token(const PagedFewArgs& f, int rr) {
+    return f.a.rep == 1 ? rr : static_cast<int>(__umulhi(static_cast<uint32_t>(rr), f.rep_mul));
+}
+
 // Row r (0 .. 15) of row group g of a piece: token row and position, query head.  live: it exists.
 struct FewRow {
     int t, pos, h;
     bool live;
 };
 __device__ __forceinline__ FewRow few_row(const PagedFewArgs& f, const FewSeq& q, int kv_head, int group, int r) {
-    const int rr = group * f.rows_per_group + r, i = rr / f.a.rep;
+    const int rr = group * f.rows_per_group + r, i = few_token(f, rr);
     FewRow o;
     o.live = r < f.rows_per_group && i < q.s.n;
     o.t = q.s.row0 + i;
@@ -284,11 +304,11 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
     __syncthreads();
     FewWalk con;
     con.b = scratch.start.b;
-    con.q = few_seq(f, con.b, false);
+    con.q = scratch.start.q;
     {
         const int64_t u = lo - scratch.start.before;
         const int per_item = con.q.tiles + kFewItemCost;
-        con.item = static_cast<int>(u / per_item);
+        con.item = static_cast<int>(few_quotient(u, per_item));
         con.left = hi - lo;
         con.more = true;
         if (!con.cut(static_cast<int>(u - static_cast<int64_t>(con.item) * per_item))) con.next(f);
@@ -297,37 +317,35 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
     // ---- the ring's filling side: chunk after chunk of this warp, across pieces
     FewWalk pro = con;
     int pk = 0, pn = pro.more ? pro.chunks(warp) : 0, p_stage = 0;
-    int64_t p_off = -1;  // lane j < 16: offset of the next chunk's position j; -1: leave out
     // the item's query rows into L1, a line of 128 bytes per lane: they are wanted as soon as its first chunk is there
     auto warm_queries = [&](const FewWalk& w) {
         constexpr int LINES = D * (QF32 ? 4 : 2) / 128;
-        const int groups = w.q.items / f.a.w.n_kv, kv_head = w.item / groups;
         for (int x = lane; x < (PACK ? 8 : 16) * LINES; x += 32) {
-            const FewRow r = few_row(f, w.q, kv_head, w.item - kv_head * groups, x / LINES);
+            const FewRow r = few_row(f, w.q, w.kv_head, w.group, x / LINES);
             if (r.live) {
                 const char* at = f.a.q + (r.t * f.a.ldq + static_cast<int64_t>(r.h) * D) * (QF32 ? 4 : 2) + x % LINES * 128;
                 asm volatile("prefetch.global.L1 [%0];" ::"l"(at));
             }
         }
     };
-    auto look_up = [&]() {
+    // lane j < 16: offset of position j of the next chunk (-1: leave out); moves on
+    auto look_up = [&]() -> int64_t {
         while (pro.more && pk >= pn) {
             pro.next(f);
             pk = 0;
             pn = pro.more ? pro.chunks(warp) : 0;
             if (pro.more) warm_queries(pro);
         }
-        if (!pro.more) return;
+        if (!pro.more) return -2;
         const int v = pro.t0 * kFewTile + (pk * kFewWarps + warp) * kFewChunk + (lane & 15);
-        p_off = -1;
-        if (v < pro.q.nv) {
-            const int groups = pro.q.items / f.a.w.n_kv;
-            p_off = paged_row(f.a.w, pro.b, few_pos(pro.q, v), pro.item / groups);
-            if (p_off < 0) report_status(f.a.w.status, AFX_ERR_INVALID_ARG);
-        }
+        ++pk;
+        if (v >= pro.q.nv) return -1;
+        const int64_t at = paged_row(f.a.w, pro.b, few_pos(pro.q, v), pro.kv_head);
+        if (at < 0) report_status(f.a.w.status, AFX_ERR_INVALID_ARG);
+        return at;
     };
-    auto issue = [&]() {
-        if (pro.more) {
+    auto issue = [&](int64_t p_off) {  // (-2: no chunk; the same for all lanes)
+        if (p_off != -2) {
             const uint32_t at = ring + p_stage * Cfg::kChunkBytes;
             const uint32_t mask = __ballot_sync(0xFFFFFFFFu, p_off >= 0) & 0xFFFFu;
             if (lane == 0) stage_mask[warp][p_stage] = mask;
@@ -342,19 +360,23 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                 few_copy16(d + kFewChunk * D * 2, f.a.w.v + e, off < 0 ? 0 : 16);
             }
             p_stage = p_stage + 1 == ST ? 0 : p_stage + 1;
-            ++pk;
-            look_up();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    look_up();
+    int64_t ahead;  // the chunk behind those on their way: looked up a chunk's time before it is wanted
+    {
+        int64_t off[ST - 1];
 #pragma unroll
-    for (int i = 0; i < ST - 1; ++i) issue();
+        for (int i = 0; i < ST - 1; ++i) off[i] = look_up();
+        ahead = look_up();
+#pragma unroll
+        for (int i = 0; i < ST - 1; ++i) issue(off[i]);
+    }
 
     int stage = 0;
     for (; con.more; con.next(f)) {
         const FewSeq& q = con.q;
-        const int groups = q.items / f.a.w.n_kv, kv_head = con.item / groups, group = con.item - kv_head * groups;
+        const int kv_head = con.kv_head, group = con.group;
         // ---- queries of the lane's rows as fragments of the first product
         uint32_t qa[NK][4], ql[QF32 && !PACK ? NK : 1][4];
         float unit[NR];
@@ -514,7 +536,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
             }
             __syncwarp();
             stage = stage + 1 == ST ? 0 : stage + 1;
-            issue();
+            issue(ahead);
+            ahead = look_up();
         }
 
         // ---- the warps' sums meet
@@ -670,7 +693,7 @@ __global__ void __launch_bounds__(kFewThreads) paged_join_kernel(PagedFewArgs f)
             s.w = fmaf(s.w, wa, t[u].w * wb);
         }
     }
-    const int rr = j.first + r, i = rr / f.a.rep;
+    const int rr = j.first + r, i = few_token(f, rr);
     few_store<D>(f, j.row0 + i, j.h0 + rr - i * f.a.rep, d, s, M, L);
 }
 
