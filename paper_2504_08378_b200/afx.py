@@ -485,17 +485,16 @@ def afx_layer_step_hosted(model: int, layer: int, state: int, pos: int, ops: Hos
 def afx_paged_append(kv: PagedKV, prep: HeadPrep, q, ldq: int, k, ldk: int, v, ldv: int, q_out, q_out_dtype, stream=None,
                      dev_status=None):
     _check("afx_paged_append",
-           lib().afx_paged_append(ctypes.byref(kv), ctypes.byref(prep), _ptr(q), int(ldq), _ptr(k), int(ldk), _ptr(v), int(ldv),
-                                  _ptr(q_out), _dt(q_out_dtype), _ptr(dev_status), _stream(stream)))
+           lib().afx_paged_append(kv, prep, _ptr(q), ldq, _ptr(k), ldk, _ptr(v), ldv, _ptr(q_out), _dt(q_out_dtype),
+                                  _ptr(dev_status), _stream(stream)))
 
 
 def afx_paged_attn_workspace_bytes(kv: PagedKV, n_heads: int) -> int:
-    return int(lib().afx_paged_attn_workspace_bytes(ctypes.byref(kv), int(n_heads)))
+    return int(lib().afx_paged_attn_workspace_bytes(kv, n_heads))
 
 
 def afx_paged_attn(kv: PagedKV, q, q_dtype, ldq: int, n_heads: int, scale: float, window: int, sinks: int, out, out_dtype,
                    lse=None, workspace=None, workspace_bytes: int = 0, stream=None, dev_status=None):
     _check("afx_paged_attn",
-           lib().afx_paged_attn(ctypes.byref(kv), _ptr(q), _dt(q_dtype), int(ldq), int(n_heads), float(scale), int(window),
-                                int(sinks), _ptr(out), _dt(out_dtype), _ptr(lse), _ptr(workspace), int(workspace_bytes),
-                                _ptr(dev_status), _stream(stream)))
+           lib().afx_paged_attn(kv, _ptr(q), _dt(q_dtype), ldq, n_heads, scale, window, sinks, _ptr(out), _dt(out_dtype),
+                                _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(dev_status), _stream(stream)))

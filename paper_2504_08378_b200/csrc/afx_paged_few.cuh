@@ -26,14 +26,20 @@ constexpr int kFewChunk = 16;
 constexpr int kFewTile = kFewChunk * kFewWarps;
 constexpr int kFewMaxBlocks = 296;  // ranges at most (two blocks on each of 148 SMs); sizes the workspace
 constexpr int kFewRows = 16;
+constexpr int kOneWarps = 8, kOneCluster = 16;  // one sequence: warps of a block, blocks of a cluster at most
 
 template <int D>
 struct FewCfg {
     static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr int kChunkBytes = 2 * kFewChunk * D * 2;  // K rows, V rows
-    static constexpr int kRing = kFewWarps * kStages * kChunkBytes;
+    static constexpr int kWarpRing = kStages * kChunkBytes;
+    static constexpr int kRing = kFewWarps * kWarpRing;
     static constexpr int kMerge = kFewWarps * 1024 * 4;        // [warp][1024 values of the partial outputs]
     static constexpr int kDyn = kRing + kMerge;
+    // one sequence: the rings (where the warps' sums meet too, in the end), and the cluster's sums
+    static constexpr int kOneRing = kOneWarps * kWarpRing;
+    static constexpr int kOneRecv = (16 * D / 4 + kOneCluster) * 16;
+    static constexpr int kOneDyn = kOneRing + kOneRecv + 2 * kOneCluster * 16 * 4;
 };
 
 // What an item costs beside its tiles (queries, the warps' sums), in tiles: the ranges are cut with it counted in.
@@ -167,15 +173,18 @@ struct FewWalk {
     int64_t left;       // units of the range behind this piece
     bool more;          // there is a piece
 
+    __device__ __forceinline__ void place() {
+        kv_head = item;
+        if (q.groups > 1) kv_head = static_cast<int>(static_cast<uint32_t>(item) / static_cast<uint32_t>(q.groups));
+        group = item - kv_head * q.groups;
+    }
     // The piece from unit u0 of the item on; false where the range ends in front of its tiles.
     __device__ __forceinline__ bool cut(int u0) {
         const int u1 = static_cast<int>(min(static_cast<int64_t>(q.tiles + kFewItemCost), u0 + left));
         left -= u1 - u0;
         t0 = max(u0 - kFewItemCost, 0);
         t1 = max(u1 - kFewItemCost, 0);
-        kv_head = item;
-        if (q.groups > 1) kv_head = static_cast<int>(static_cast<uint32_t>(item) / static_cast<uint32_t>(q.groups));
-        group = item - kv_head * q.groups;
+        place();
         return t1 > t0 || q.tiles == 0;
     }
     __device__ __forceinline__ void next(const PagedFewArgs& f) {
@@ -196,10 +205,11 @@ struct FewWalk {
             }
         } while (!cut(0));
     }
-    // chunks of this piece that warp w takes: w, w + warps, ..
+    // chunks of this piece that warp w of W takes: w, w + W, ..
+    template <int W>
     __device__ __forceinline__ int chunks(int w) const {
-        const int n = (min(q.nv, t1 * kFewTile) - t0 * kFewTile + kFewChunk - 1) / kFewChunk;
-        return n > w ? (n - w + kFewWarps - 1) / kFewWarps : 0;
+        const int n = (min(q.nv, t1 * (W * kFewChunk)) - t0 * (W * kFewChunk) + kFewChunk - 1) / kFewChunk;
+        return n > w ? (n - w + W - 1) / W : 0;
     }
 };
 
@@ -275,37 +285,61 @@ __device__ __forceinline__ void few_store(const PagedFewArgs& f, int t, int h, i
     if (f.a.lse != nullptr && d == 0) f.a.lse[at] = none ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
-template <int D, int CT, bool PACK, bool QF32>
-__global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs f) {
+// ONE: the cache of one sequence.  All its items have the same length, so that a cluster of blocks takes an item, a block an
+// equal share of its tiles (8 warps and the whole SM), and the sums meet through distributed shared memory: one kernel, no
+// list, no workspace.  grid (blocks of a cluster, items).
+template <int D, int CT, bool PACK, bool QF32, bool ONE>
+__global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 2) paged_few_kernel(PagedFewArgs f) {
     using Cfg = FewCfg<D>;
+    constexpr int W = ONE ? kOneWarps : kFewWarps, THREADS = W * 32;
     constexpr int ST = Cfg::kStages, NK = D / 16, NT = D / 8, PIECES = D / 8;
     constexpr int NR = PACK ? 1 : 2;                       // rows of a lane: gid (and gid + 8)
     constexpr float kUp = CT == AFX_F16 ? 1024.0f : 1.0f;  // weights are carried times this: the low halves of small ones stay normal
     extern __shared__ __align__(128) unsigned char dyn[];
-    __shared__ uint32_t stage_mask[kFewWarps][ST];
-    __shared__ float sm_m[kFewWarps][kFewRows], sm_l[kFewWarps][kFewRows];
+    __shared__ uint32_t stage_mask[W][ST];
+    __shared__ float sm_m[W][kFewRows], sm_l[W][kFewRows];
     __shared__ FewScratch scratch;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int gid = lane >> 2, tig = lane & 3;
-    float* merge = reinterpret_cast<float*>(dyn + Cfg::kRing);
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dyn)) + warp * ST * Cfg::kChunkBytes;
+    // where warp w's sums meet the others': behind the rings, or in its ring, which is empty by then
+    auto merge = [&](int w) { return reinterpret_cast<float*>(dyn + (ONE ? w * Cfg::kWarpRing : Cfg::kRing + w * 4096)); };
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dyn)) + warp * Cfg::kWarpRing;
 
+    if constexpr (ONE) cluster_arrive();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    int64_t mine_before, mine;
-    const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine);
-    const FewRanges ranges(total, gridDim.x);
-    const int my = blockIdx.x;
-    if (tid == 0) f.joins[my].last = -1;  // (a later piece may say otherwise)
-    if (my >= ranges.n) return;
-    const int64_t lo = ranges.begin(my), hi = ranges.begin(my + 1);
-    few_find(f, &scratch, lo, mine_before, mine);
-    __syncthreads();
+    const int my = blockIdx.x;  // range, or rank in the cluster
     FewWalk con;
-    con.b = scratch.start.b;
-    con.q = scratch.start.q;
-    {
+    FewRanges ranges(0, 1);
+    int64_t hi = 0;
+    if constexpr (ONE) {
+        con.b = 0;
+        con.q = few_seq(f, 0, blockIdx.x == 0 && blockIdx.y == 0);
+        con.item = blockIdx.y;
+        if (con.item >= con.q.items) {  // (the same for the cluster)
+            cluster_wait();
+            return;
+        }
+        con.q.tiles = (con.q.nv + W * kFewChunk - 1) / (W * kFewChunk);
+        const int64_t S = gridDim.x;
+        con.place();
+        con.t0 = static_cast<int>(static_cast<uint32_t>(my * con.q.tiles) / static_cast<uint32_t>(S));
+        con.t1 = static_cast<int>(static_cast<uint32_t>((my + 1) * con.q.tiles) / static_cast<uint32_t>(S));
+        con.left = 0;
+        con.more = true;
+    } else {
+        int64_t mine_before, mine;
+        const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine);
+        ranges = FewRanges(total, gridDim.x);
+        if (tid == 0) f.joins[my].last = -1;  // (a later piece may say otherwise)
+        if (my >= ranges.n) return;
+        const int64_t lo = ranges.begin(my);
+        hi = ranges.begin(my + 1);
+        few_find(f, &scratch, lo, mine_before, mine);
+        __syncthreads();
+        con.b = scratch.start.b;
+        con.q = scratch.start.q;
         const int64_t u = lo - scratch.start.before;
         const int per_item = con.q.tiles + kFewItemCost;
         con.item = static_cast<int>(few_quotient(u, per_item));
@@ -316,7 +350,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
 
     // ---- the ring's filling side: chunk after chunk of this warp, across pieces
     FewWalk pro = con;
-    int pk = 0, pn = pro.more ? pro.chunks(warp) : 0, p_stage = 0;
+    int pk = 0, pn = pro.more ? pro.chunks<W>(warp) : 0, p_stage = 0;
     // the item's query rows into L1, a line of 128 bytes per lane: they are wanted as soon as its first chunk is there
     auto warm_queries = [&](const FewWalk& w) {
         constexpr int LINES = D * (QF32 ? 4 : 2) / 128;
@@ -333,11 +367,11 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
         while (pro.more && pk >= pn) {
             pro.next(f);
             pk = 0;
-            pn = pro.more ? pro.chunks(warp) : 0;
+            pn = pro.more ? pro.chunks<W>(warp) : 0;
             if (pro.more) warm_queries(pro);
         }
         if (!pro.more) return -2;
-        const int v = pro.t0 * kFewTile + (pk * kFewWarps + warp) * kFewChunk + (lane & 15);
+        const int v = ((pro.t0 + pk) * W + warp) * kFewChunk + (lane & 15);
         ++pk;
         if (v >= pro.q.nv) return -1;
         const int64_t at = paged_row(f.a.w, pro.b, few_pos(pro.q, v), pro.kv_head);
@@ -435,9 +469,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
 #pragma unroll
             for (int x = 0; x < 4; ++x) o[i][x] = 0.0f;
         const int last = q.s.first + q.s.n - 1;
-        const int n_chunks = con.chunks(warp);
+        const int n_chunks = con.chunks<W>(warp);
         for (int k = 0; k < n_chunks; ++k) {
-            const int v0 = con.t0 * kFewTile + (k * kFewWarps + warp) * kFewChunk;
+            const int v0 = ((con.t0 + k) * W + warp) * kFewChunk;
             asm volatile("cp.async.wait_group %0;" ::"n"(ST - 2) : "memory");
             __syncwarp();
             const uint32_t kat = ring + stage * Cfg::kChunkBytes, vat = kat + kFewChunk * D * 2;
@@ -568,9 +602,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                 sm_l[warp][gid + 8 * e] = l[e] * (1.0f / kUp);
             }
         }
-        const bool whole_item = con.t0 == 0 && con.t1 == q.tiles;
-        float* slot = f.slots + static_cast<int64_t>(2 * my + (con.t0 > 0 ? 0 : 1)) * few_slot_floats(D);
-        if (!whole_item && con.t0 == 0 && tid == 0) {  // this range has the item joined
+        const bool whole_item = !ONE && con.t0 == 0 && con.t1 == q.tiles;
+        float* slot = ONE ? nullptr : f.slots + static_cast<int64_t>(2 * my + (con.t0 > 0 ? 0 : 1)) * few_slot_floats(D);
+        if (!ONE && !whole_item && con.t0 == 0 && tid == 0) {  // this range has the item joined
             const int64_t end = hi + (q.tiles - con.t1);   // (its piece ends the range)
             const int first = group * f.rows_per_group;
             FewJoin j = {};
@@ -585,7 +619,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
         constexpr int RW = PACK ? 8 : 16, DW = PACK ? D : 64;
 #pragma unroll
         for (int part = 0; part < D / DW; ++part) {
-            float* mine = merge + warp * 1024;
+            float* mine = merge(warp);
 #pragma unroll
             for (int i = 0; i < DW / 8; ++i)
 #pragma unroll
@@ -605,7 +639,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                     qv[x] = fr.live ? f.a.scale * typed_value(f.a.q, f.a.q_type, fr.t * f.a.ldq + static_cast<int64_t>(fr.h) * D + lane * (D / 32) + x) : 0.0f;
                 }
                 for (int k = 0; fr.live && k < n_chunks; ++k) {
-                    const int v0 = con.t0 * kFewTile + (k * kFewWarps + warp) * kFewChunk;
+                    const int v0 = ((con.t0 + k) * W + warp) * kFewChunk;
                     for (int v = v0; v < min(v0 + kFewChunk, q.nv); ++v) {
                         const int p = few_pos(q, v);
                         if (few_sees(f.a.mask, fr.pos, p)) attend_row<D, CT>(f.a.w, con.b, kv_head, qv, p, p + 1, st);
@@ -622,20 +656,21 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                 }
                 __syncwarp();
             }
+            if (ONE && part == 0) cluster_wait();  // the peers are running
             __syncthreads();
             // four neighbouring dims of a row per thread and turn
-            for (int x = tid * 4; x < RW * DW; x += kFewThreads * 4) {
+            for (int x = tid * 4; x < RW * DW; x += THREADS * 4) {
                 const int r = x / DW, d = part * DW + x % DW;
                 const FewRow fr = few_row(f, q, kv_head, group, r);
                 if (!fr.live) continue;
                 float M = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < kFewWarps; ++w) M = fmaxf(M, sm_m[w][r]);
+                for (int w = 0; w < W; ++w) M = fmaxf(M, sm_m[w][r]);
                 float L = 0.0f;
                 float4 s4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                for (int w = 0; w < kFewWarps; ++w) {
-                    const float4 t = *reinterpret_cast<const float4*>(merge + w * 1024 + x);
+                for (int w = 0; w < W; ++w) {
+                    const float4 t = *reinterpret_cast<const float4*>(merge(w) + x);
                     const float wt = sm_m[w][r] == -INFINITY ? 0.0f : fast_exp2(sm_m[w][r] - M);
                     if (wt == 0.0f && sm_l[w][r] == 0.0f) continue;
                     L = fmaf(wt, sm_l[w][r], L);
@@ -644,7 +679,17 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                     s4.z = fmaf(wt, t.z, s4.z);
                     s4.w = fmaf(wt, t.w, s4.w);
                 }
-                if (whole_item) {
+                if constexpr (ONE) {  // block e % S of the cluster finishes the e-th four values
+                    cg::cluster_group cluster = cg::this_cluster();
+                    const int S = gridDim.x, e = (r * D + d) / 4, per = (RW * D / 4 + S - 1) / S;
+                    float4* recv = reinterpret_cast<float4*>(dyn + Cfg::kOneRing);
+                    cluster.map_shared_rank(recv, e % S)[my * per + e / S] = s4;
+                    if (d / 4 < S) {
+                        float* ml = cluster.map_shared_rank(reinterpret_cast<float*>(dyn + Cfg::kOneRing + Cfg::kOneRecv), d / 4);
+                        ml[my * kFewRows + r] = M;
+                        ml[(kOneCluster + my) * kFewRows + r] = L;
+                    }
+                } else if (whole_item) {
                     few_store<D>(f, fr.t, fr.h, d, s4, M, L);
                 } else {
                     *reinterpret_cast<float4*>(slot + 2 * kFewRows + r * D + d) = s4;
@@ -655,6 +700,35 @@ __global__ void __launch_bounds__(kFewThreads, 2) paged_few_kernel(PagedFewArgs 
                 }
             }
             __syncthreads();
+        }
+    }
+    if constexpr (ONE) {
+        cluster_arrive();
+        cluster_wait();
+        const FewSeq& q = con.q;
+        constexpr int RW = PACK ? 8 : 16;
+        const int S = gridDim.x, per = (RW * D / 4 + S - 1) / S;
+        const float4* recv = reinterpret_cast<const float4*>(dyn + Cfg::kOneRing);
+        const float* ml = reinterpret_cast<const float*>(dyn + Cfg::kOneRing + Cfg::kOneRecv);
+        for (int i = tid; my + S * i < RW * D / 4; i += THREADS) {
+            const int e = (my + S * i) * 4, r = e / D, d = e % D;
+            const FewRow fr = few_row(f, q, con.kv_head, con.group, r);
+            if (!fr.live) continue;
+            float M = -INFINITY, L = 0.0f;
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int k = 0; k < S; ++k) M = fmaxf(M, ml[k * kFewRows + r]);
+            for (int k = 0; k < S; ++k) {
+                const float m = ml[k * kFewRows + r], l = ml[(kOneCluster + k) * kFewRows + r];
+                if (m == -INFINITY && l == 0.0f) continue;  // (nothing seen there)
+                const float wt = fast_exp2(m - M);
+                const float4 t = recv[k * per + i];
+                L = fmaf(wt, l, L);
+                s.x = fmaf(wt, t.x, s.x);
+                s.y = fmaf(wt, t.y, s.y);
+                s.z = fmaf(wt, t.z, s.z);
+                s.w = fmaf(wt, t.w, s.w);
+            }
+            few_store<D>(f, fr.t, fr.h, d, s, M, L);
         }
     }
 }
