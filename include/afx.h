@@ -47,8 +47,9 @@ typedef int32_t afx_status;
 #define AFX_ERR_CAPACITY 3    /* a caller-provided buffer or a fixed limit is too small */
 #define AFX_ERR_UNSUPPORTED 4 /* unknown dtype or mode */
 #define AFX_ERR_CUDA 5        /* the CUDA runtime refused a launch or a query */
-#define AFX_ERR_TIMEOUT 6     /* reserved: a bounded device-side wait gave up.  No kernel of this */
-                              /* version waits on a flag, so nothing returns or stores it.        */
+#define AFX_ERR_TIMEOUT 6     /* a bounded device-side wait gave up (dev_status of a prompt's     */
+                              /* attention; its waits are for its own copies and products, and no */
+                              /* call of a working GPU comes near their limit)                    */
 
 #define AFX_F16 0
 #define AFX_BF16 1
@@ -227,8 +228,8 @@ typedef struct {
     const void* w_down; /* [mlp][hidden]                                                       */
     const float* g_attn; /* [hidden] fp32 RMSNorm gains                                        */
     const float* g_mlp;
-    void* k_cache;      /* [T][max_seq][n_kv_heads][128] fp16, one cache per token stream      */
-    void* v_cache;
+    void* k_cache;      /* [T][max_seq][n_kv_heads][128] fp16, one cache per token stream; both */
+    void* v_cache;      /* NULL: the layer is only stepped by afx_layer_step_paged              */
     int32_t k[4];       /* per AFX_OP_*: channels kept in top-k mode                           */
     float tau[4];       /* per AFX_OP_*: threshold in threshold mode                           */
 } afx_layer_desc;
@@ -758,7 +759,7 @@ size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads);
  *
  * of the token's sequence and kv head h / (n_heads / n_kv_heads).  With the token at position p, j is visible when
  * j <= p and (window = 0, or j > p - window, or j < sinks): a sliding window and a few first positions that stay visible.
- * A token that sees nothing gets zeros (lse: -inf).  What lies at positions that no token sees, or that only other tokens
+ * A token that sees nothing, or only scores of -inf, gets zeros (lse: -inf).  What lies at positions that no token sees, or that only other tokens
  * see, has no influence (NaN and infinities included).
  *
  *   q         DEVICE rows of n_heads * head_dim values, ldq values from row to row (a multiple of 8), 16-byte aligned; q_dtype = the
@@ -772,6 +773,23 @@ size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads);
 afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads, float scale,
                           int window, int sinks, void* out, int out_dtype, float* lse, void* workspace,
                           size_t workspace_bytes, int32_t* dev_status, void* stream);
+
+/*
+ * afx_layer_step over a paged cache, for the T token rows of the state: T sequences with a new token each, every one at its
+ * own position, or fewer sequences with several new tokens (kv->n_tokens = T; rows behind the last sequence pass through the
+ * operators but see nothing: their attention output keeps what AFX_BUF_ATTN held).  The kernels of afx_layer_step with the
+ * attention replaced: q | k | v operator, afx_paged_append (the model's rotary table; per-head norms where gains are given, eps as the
+ * model's; positions below max_seq), afx_paged_attn on the unrounded fp32 queries, o, gate/up and down operators.  Cross-layer modes
+ * as in afx_layer_step.
+ *
+ *   kv        n_kv_heads and head_dim as the model's; its pages belong to THIS layer; dtype of its own.
+ *   window, sinks, dev_status   as for afx_paged_attn;  g_q, g_k  as in afx_head_prep (NULL: no norm).
+ *   workspace DEVICE, afx_layer_paged_workspace_bytes, 256-byte aligned; not shared with a call that may overlap.
+ */
+size_t afx_layer_paged_workspace_bytes(const afx_model* model, const afx_paged_kv* kv);
+afx_status afx_layer_step_paged(afx_model* model, int layer, afx_state* state, const afx_paged_kv* kv, int window,
+                                int sinks, const float* g_q, const float* g_k, void* workspace, size_t workspace_bytes,
+                                int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

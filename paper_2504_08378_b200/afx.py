@@ -211,6 +211,10 @@ def lib() -> ctypes.CDLL:
         L.afx_paged_attn_workspace_bytes.argtypes = [ctypes.POINTER(PagedKV), c_int]
         L.afx_paged_attn.argtypes = [ctypes.POINTER(PagedKV), c_void_p, c_int, c_int64, c_int, c_float, c_int, c_int,
                                      c_void_p, c_int, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+        L.afx_layer_paged_workspace_bytes.restype = c_size_t
+        L.afx_layer_paged_workspace_bytes.argtypes = [c_void_p, ctypes.POINTER(PagedKV)]
+        L.afx_layer_step_paged.argtypes = [c_void_p, c_int, c_void_p, ctypes.POINTER(PagedKV), c_int, c_int, c_void_p, c_void_p,
+                                           c_void_p, c_size_t, c_void_p, c_void_p]
         _lib = L
     return _lib
 
@@ -498,3 +502,14 @@ def afx_paged_attn(kv: PagedKV, q, q_dtype, ldq: int, n_heads: int, scale: float
     _check("afx_paged_attn",
            lib().afx_paged_attn(kv, _ptr(q), _dt(q_dtype), ldq, n_heads, scale, window, sinks, _ptr(out), _dt(out_dtype),
                                 _ptr(lse), _ptr(workspace), workspace_bytes, _ptr(dev_status), _stream(stream)))
+
+
+def afx_layer_paged_workspace_bytes(model: int, kv: PagedKV) -> int:
+    return int(lib().afx_layer_paged_workspace_bytes(model, kv))
+
+
+def afx_layer_step_paged(model: int, layer: int, state: int, kv: PagedKV, window: int, sinks: int, g_q, g_k, workspace,
+                         workspace_bytes: int, stream=None, dev_status=None):
+    _check("afx_layer_step_paged",
+           lib().afx_layer_step_paged(model, layer, state, kv, window, sinks, _ptr(g_q), _ptr(g_k), _ptr(workspace),
+                                      workspace_bytes, _ptr(dev_status), _stream(stream)))

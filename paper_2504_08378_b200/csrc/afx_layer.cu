@@ -189,9 +189,9 @@ extern "C" afx_status afx_model_create(const afx_model_desc* desc, const afx_lay
     const int K_op[4] = {d.hidden, d.n_heads * d.head_dim, d.hidden, d.mlp};
     for (int l = 0; l < d.n_layers; ++l) {
         const afx_layer_desc& L = layers[l];
-        // (a NULL weight pointer is allowed: the operator must then come from a host handle or 4-bit rows)
-        if (L.g_attn == nullptr || L.g_mlp == nullptr || L.k_cache == nullptr || L.v_cache == nullptr)
-            return AFX_ERR_INVALID_ARG;
+        // (a NULL weight pointer is allowed: the operator must then come from a host handle or 4-bit rows; NULL caches are: the
+        // layer is then only stepped over a paged cache)
+        if (L.g_attn == nullptr || L.g_mlp == nullptr || (L.k_cache == nullptr) != (L.v_cache == nullptr)) return AFX_ERR_INVALID_ARG;
         if (!aligned16(L.w_qkv) || !aligned16(L.w_o) || !aligned16(L.w_gu) || !aligned16(L.w_down) ||
             !aligned16(L.k_cache) || !aligned16(L.v_cache) || !aligned16(L.g_attn) || !aligned16(L.g_mlp))
             return AFX_ERR_ALIGNMENT;
@@ -344,10 +344,11 @@ static void plan_selection(const afx_model* m, const afx_state* s, int layer, in
     if (predictor) a->bitmap_out = reinterpret_cast<uint32_t*>(s->blob + s->off_pred[op][(layer / depth) & 1]);
 }
 
-static afx_status check_step(const afx_model* m, int layer, const afx_state* s) {
+static afx_status check_step(const afx_model* m, int layer, const afx_state* s, bool own_cache = true) {
     if (m == nullptr || s == nullptr) return AFX_ERR_INVALID_ARG;
     if (s->model != m) return AFX_ERR_INVALID_ARG;
     if (layer < 0 || layer >= m->d.n_layers) return AFX_ERR_INVALID_ARG;
+    if (own_cache && m->layers[layer].k_cache == nullptr) return AFX_ERR_INVALID_ARG;
     return AFX_OK;
 }
 
@@ -451,7 +452,7 @@ extern "C" afx_status afx_layer_step(afx_model* m, int layer, afx_state* s, int 
 
 extern "C" afx_status afx_layer_kernel(afx_model* m, int layer, afx_state* s, int pos, int which, void* stream) {
     using namespace afx;
-    afx_status rc = check_step(m, layer, s);
+    afx_status rc = check_step(m, layer, s, which == AFX_STEP_ATTN);
     if (rc != AFX_OK) return rc;
     if (pos < 0 || pos >= m->d.max_seq || which < AFX_STEP_QKV || which > AFX_STEP_DOWN) return AFX_ERR_INVALID_ARG;
     return launch_layer_kernel(m, layer, s, pos, which, false, static_cast<cudaStream_t>(stream));
@@ -611,10 +612,70 @@ extern "C" afx_status afx_layer_step_q4(afx_model* m, int layer, afx_state* s, i
     return AFX_OK;
 }
 
+extern "C" size_t afx_layer_paged_workspace_bytes(const afx_model* m, const afx_paged_kv* kv) {
+    if (m == nullptr || kv == nullptr) return 0;
+    const size_t attn = afx_paged_attn_workspace_bytes(kv, m->d.n_heads);
+    if (attn == 0 || kv->n_tokens > AFX_MAX_T) return 0;
+    return attn + afx::align256(static_cast<size_t>(kv->n_tokens) * m->d.n_heads * m->d.head_dim * sizeof(float));
+}
+
+extern "C" afx_status afx_layer_step_paged(afx_model* m, int layer, afx_state* s, const afx_paged_kv* kv, int window,
+                                           int sinks, const float* g_q, const float* g_k, void* workspace,
+                                           size_t workspace_bytes, int32_t* dev_status, void* stream) {
+    using namespace afx;
+    afx_status rc = check_step(m, layer, s, false);
+    if (rc != AFX_OK) return rc;
+    if (kv == nullptr || workspace == nullptr) return AFX_ERR_INVALID_ARG;
+    const afx_model_desc& d = m->d;
+    const afx_layer_desc& L = m->layers[layer];
+    if (kv->n_tokens != s->T || kv->n_kv_heads != d.n_kv_heads || kv->head_dim != d.head_dim || kv->max_new > s->T) return AFX_ERR_INVALID_ARG;
+    if (L.w_qkv == nullptr || L.w_o == nullptr || L.w_gu == nullptr || L.w_down == nullptr) return AFX_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return AFX_ERR_ALIGNMENT;
+    if (kv->tok_start == nullptr && (kv->max_new != 1 || kv->n_tokens < kv->n_seqs)) return AFX_ERR_INVALID_ARG;
+    if (kv->n_seqs < 0) return AFX_ERR_INVALID_ARG;
+    if (kv->n_seqs > 65535) return AFX_ERR_CAPACITY;
+    const size_t attn_bytes = afx_paged_attn_workspace_bytes(kv, d.n_heads);
+    if (attn_bytes != 0 && workspace_bytes < afx_layer_paged_workspace_bytes(m, kv)) return AFX_ERR_CAPACITY;
+    afx_head_prep prep = {};
+    prep.x_dtype = AFX_F32;
+    prep.n_heads = d.n_heads;
+    prep.eps = d.rms_eps;
+    prep.rope_style = AFX_ROPE_PAIRS;
+    prep.rotary_dim = d.head_dim;
+    prep.rope_len = d.max_seq;
+    prep.g_q = g_q;
+    prep.g_k = g_k;
+    prep.rope_cos = m->rope;
+    prep.rope_sin = m->rope + static_cast<size_t>(d.max_seq) * (kHeadDim / 2);
+    const float* q = reinterpret_cast<const float*>(s->blob + s->off_qkv);
+    const float* k = q + static_cast<size_t>(d.n_heads) * d.head_dim;
+    const float* v = k + static_cast<size_t>(d.n_kv_heads) * d.head_dim;
+    float* rotated = reinterpret_cast<float*>(static_cast<char*>(workspace) + attn_bytes);
+    void* attn = s->blob + s->off_attn;
+    const int64_t ldq = static_cast<int64_t>(d.n_heads) * d.head_dim;
+    auto append = [&](const afx_paged_kv& c) {
+        return afx_paged_append(&c, &prep, q, m->n_qkv, k, m->n_qkv, v, m->n_qkv, rotated, AFX_F32, dev_status, stream);
+    };
+    auto attend = [&](const afx_paged_kv& c) {
+        return afx_paged_attn(&c, rotated, AFX_F32, ldq, d.n_heads, 0.0f, window, sinks, attn, d.dtype, nullptr, workspace, attn_bytes,
+                              dev_status, stream);
+    };
+    // both calls' checks (without sequences they launch nothing) before anything is enqueued
+    afx_paged_kv none = *kv;
+    none.n_seqs = 0;
+    if ((rc = append(none)) != AFX_OK || (rc = attend(none)) != AFX_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((rc = launch_layer_kernel(m, layer, s, 0, AFX_STEP_QKV, true, st)) != AFX_OK) return rc;
+    if ((rc = append(*kv)) != AFX_OK || (rc = attend(*kv)) != AFX_OK) return rc;
+    for (int which = AFX_STEP_O; which <= AFX_STEP_DOWN; ++which)
+        if ((rc = launch_layer_kernel(m, layer, s, 0, which, true, st)) != AFX_OK) return rc;
+    return AFX_OK;
+}
+
 extern "C" afx_status afx_mlp_block(afx_model* m, int layer, afx_state* s, const void* x, float* y,
                                     void* stream) {
     using namespace afx;
-    afx_status rc = check_step(m, layer, s);
+    afx_status rc = check_step(m, layer, s, false);
     if (rc != AFX_OK) return rc;
     if (x == nullptr || y == nullptr) return AFX_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(x) & 1u) != 0 || !aligned16(y)) return AFX_ERR_ALIGNMENT;

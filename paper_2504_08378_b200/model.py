@@ -29,11 +29,13 @@ class DecoderModel:
     layers: list of dicts with numpy bit-pattern weights ``w_qkv, w_o, w_gate, w_up, w_down``,
     fp32 gains ``g_attn, g_mlp``, optional ``k`` / ``tau`` (length-4 sequences indexed by
     afx.OP_*), optional caches ``k_cache, v_cache`` ([T][max_seq][n_kv][128] uint16).
+    paged: the layers have no caches of their own and are stepped over pages (layer_step_paged).
     """
 
     def __init__(self, dtype: str, hidden: int, n_heads: int, n_kv_heads: int, mlp: int, max_seq: int,
                  layers, T: int = 1, select_mode: int = afx.MODE_TOPK, xl_depth: int = 0,
-                 xl_mode: int = afx.XL_OFF, eps: float = 1e-5, theta: float = 10000.0, head_dim: int = 128):
+                 xl_mode: int = afx.XL_OFF, eps: float = 1e-5, theta: float = 10000.0, head_dim: int = 128,
+                 paged: bool = False):
         self.dtype, self.hidden, self.n_heads, self.n_kv_heads = dtype, hidden, n_heads, n_kv_heads
         self.mlp, self.max_seq, self.T, self.head_dim = mlp, max_seq, T, head_dim
         self.n_qkv = (n_heads + 2 * n_kv_heads) * head_dim
@@ -58,7 +60,9 @@ class DecoderModel:
                     q4.ldq_bytes[op] = 0 if rows is None else rows.shape[1]
                 tens["q4"] = L["q4"]
             self.q4.append(q4)
-            if "k_cache" in L:
+            if paged:
+                kc = vc = None
+            elif "k_cache" in L:
                 kc, vc = to_device_bits(L["k_cache"]), to_device_bits(L["v_cache"])
             else:
                 kc = torch.zeros((T, max_seq, n_kv_heads, head_dim), dtype=torch.int16, device="cuda")
@@ -84,6 +88,7 @@ class DecoderModel:
         off = (-raw.data_ptr()) % 256
         self.blob = raw[off:off + nbytes]
         self.state = afx.afx_state_create(self.handle, T, self.blob, nbytes)
+        self._paged_work = None
         torch.cuda.synchronize()
 
     def close(self):
@@ -142,6 +147,20 @@ class DecoderModel:
     def decode_step(self, pos: int, stream=None):
         for layer in range(self.n_layers):
             afx.afx_layer_step(self.handle, layer, self.state, pos, stream)
+
+    def layer_step_paged(self, layer: int, kv: "afx.PagedKV", window: int = 0, sinks: int = 0, g_q=None, g_k=None, stream=None,
+                         dev_status=None):
+        """kv: this layer's pages.  The model keeps one workspace: its paged steps follow one another on the GPU."""
+        need = afx.afx_layer_paged_workspace_bytes(self.handle, kv)
+        if self._paged_work is None or self._paged_work.numel() < need + 256:
+            self._paged_work = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+        base = self._paged_work.data_ptr()
+        afx.afx_layer_step_paged(self.handle, layer, self.state, kv, window, sinks, g_q, g_k, base + -base % 256, need, stream, dev_status)
+
+    def decode_step_paged(self, kvs, window: int = 0, sinks: int = 0, stream=None, dev_status=None):
+        """kvs: one afx.PagedKV per layer."""
+        for layer, kv in enumerate(kvs):
+            self.layer_step_paged(layer, kv, window, sinks, stream=stream, dev_status=dev_status)
 
     def layer_step_q4(self, layer: int, pos: int, stream=None, dev_status=None):
         afx.afx_layer_step_q4(self.handle, layer, self.state, pos, self.q4[layer], stream, dev_status)
