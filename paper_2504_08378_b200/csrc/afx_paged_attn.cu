@@ -19,7 +19,7 @@ static afx_status attn_args(const afx_paged_kv* kv, int n_heads, int32_t* dev_st
 extern "C" size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads) {
     afx::PagedAttnArgs a = {};
     if (afx::attn_args(kv, n_heads, nullptr, &a) != AFX_OK) return 0;
-    if (kv->max_new > AFX_MAX_T) return 0;
+    if (kv->max_new > AFX_MAX_T && kv->n_seqs <= 1) return 0;
     return (afx::few_workspace_bytes(kv->head_dim) + 255) / 256 * 256;
 }
 
@@ -53,12 +53,18 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
     a.out_type = out_dtype;
     a.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (kv->max_new <= AFX_MAX_T) {
+    // Sequences with up to AFX_MAX_T new tokens are split over their positions; the tiles of 128 rows are for those
+    // with more.  A batch may have both (a few prompts' chunks beside sequences that decode): one kernel after the other, each
+    // leaving out what is the other's.
+    const bool prompts = kv->max_new > AFX_MAX_T;
+    if (!prompts || kv->n_seqs > 1) {
         PagedFewArgs f = {};
         f.a = a;
+        f.most = AFX_MAX_T;
         f.joins = static_cast<FewJoin*>(workspace);
         f.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_slots_at());
-        return launch_paged_few(kv->dtype, D, f, st);
+        const afx_status few = launch_paged_few(kv->dtype, D, f, st);
+        if (few != AFX_OK || !prompts) return few;
     }
-    return launch_paged_prompt(kv->dtype, D, a, st);
+    return launch_paged_prompt(kv->dtype, D, a, kv->n_seqs > 1 ? AFX_MAX_T : 0, st);
 }

@@ -57,7 +57,8 @@ static afx_status launch_one(const PagedFewArgs& f, int items, int sms, bool* ta
 
 template <int D, int CT, bool PACK, bool QF32>
 static afx_status launch_few(const PagedFewArgs& f, cudaStream_t st) {
-    const int items = f.a.w.n_kv * ((f.a.w.max_new * f.a.rep + f.rows_per_group - 1) / f.rows_per_group);
+    const int new_tokens = f.a.w.max_new < f.most ? f.a.w.max_new : f.most;
+    const int items = f.a.w.n_kv * ((new_tokens * f.a.rep + f.rows_per_group - 1) / f.rows_per_group);
     const int sms = sm_count() > 0 ? sm_count() : 148;
     if (f.a.w.n_seqs == 1 && items <= sms) {
         bool taken;
@@ -102,7 +103,8 @@ static afx_status launch_few_dt(const PagedFewArgs& f, bool pack, cudaStream_t s
 }
 
 afx_status launch_paged_few(int dtype, int D, PagedFewArgs& f, cudaStream_t st) {
-    const bool pack = few_packed(f.a.w.max_new, f.a.rep);
+    const int new_tokens = f.a.w.max_new < f.most ? f.a.w.max_new : f.most;
+    const bool pack = few_packed(new_tokens, f.a.rep);
     f.rows_per_group = pack ? 8 : kFewRows;
     f.rep_mul = static_cast<uint32_t>((uint64_t{1} << 32) / f.a.rep) + 1u;
     if (D == 128) return dtype == AFX_F16 ? launch_few_dt<128, AFX_F16>(f, pack, st) : launch_few_dt<128, AFX_BF16>(f, pack, st);

@@ -63,6 +63,7 @@ __host__ __device__ constexpr size_t few_workspace_bytes(int D) {
 struct PagedFewArgs {
     PagedAttnArgs a;
     int rows_per_group;  // 8 (packed) or 16
+    int most;            // sequences of more new tokens are somebody else's
     uint32_t rep_mul;    // r / rep = (r * rep_mul) >> 32 for 0 <= r < 2^16 (rep > 1)
     FewJoin* joins;
     float* slots;
@@ -83,6 +84,7 @@ struct FewSeq {
 __device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool report) {
     FewSeq q;
     q.s = paged_span(f.a.w, b, report);
+    if (q.s.n > f.most) q.s.n = 0;
     const int first = max(q.s.first, 0), end = min(q.s.len, q.s.first + q.s.n);
     q.low = paged_low(f.a.mask, first);
     q.few = paged_few(f.a.mask, q.low);

@@ -37,7 +37,7 @@ static bool pool_map(CUtensorMap* map, void* pages, int dtype, int D, const Page
 }
 
 template <int D, int CT>
-static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
+static afx_status launch_prompt(const PagedAttnArgs& a, int skip, cudaStream_t st) {
     const auto kern = paged_prompt_kernel<D, CT>;
     constexpr size_t dyn = PrCfg<D>::kDyn;
     if (!ensure_dyn_smem(reinterpret_cast<const void*>(kern), dyn)) {
@@ -47,7 +47,7 @@ static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     // sums of rows rounded up to pairs of row tiles, at most
     const int64_t pairs = static_cast<int64_t>(a.w.n_tokens) * a.rep / (kPrTiles * kPrRows) + a.w.n_seqs;
     if (pairs * a.w.n_kv > 0x7FFFFFFF) return AFX_ERR_CAPACITY;
-    PagedPromptArgs args = {a, 1};
+    PagedPromptArgs args = {a, 1, skip};
     CUtensorMap maps[2] = {};
     // (with a window the positions begin on a box's border, and the first ones end on one: small boxes leave less to mask)
     const int most = a.mask.window > 0 ? 16 : kPrPos;
@@ -72,9 +72,9 @@ static afx_status launch_prompt(const PagedAttnArgs& a, cudaStream_t st) {
     return AFX_OK;
 }
 
-afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, cudaStream_t st) {
-    if (D == 128) return dtype == AFX_F16 ? launch_prompt<128, AFX_F16>(a, st) : launch_prompt<128, AFX_BF16>(a, st);
-    return dtype == AFX_F16 ? launch_prompt<64, AFX_F16>(a, st) : launch_prompt<64, AFX_BF16>(a, st);
+afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, int skip, cudaStream_t st) {
+    if (D == 128) return dtype == AFX_F16 ? launch_prompt<128, AFX_F16>(a, skip, st) : launch_prompt<128, AFX_BF16>(a, skip, st);
+    return dtype == AFX_F16 ? launch_prompt<64, AFX_F16>(a, skip, st) : launch_prompt<64, AFX_BF16>(a, skip, st);
 }
 
 }  // namespace afx

@@ -33,10 +33,11 @@ constexpr float kPrGrow = 8.0f;  // powers of two that a row's maximum may grow 
 
 struct PagedPromptArgs {
     PagedAttnArgs a;
-    int box;  // positions of a tensor copy; 1: none are made
+    int box;   // positions of a tensor copy; 1: none are made
+    int skip;  // sequences of up to that many new tokens are somebody else's
 };
 
-afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, cudaStream_t st);  // afx_paged_prompt.cu
+afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, int skip, cudaStream_t st);  // afx_paged_prompt.cu
 
 template <int D>
 struct PrCfg {
@@ -59,9 +60,27 @@ struct PrWork {
     int tiles[2];              // tiles of positions that each row tile sees
 };
 
-__device__ __forceinline__ int pr_row_tiles(const PagedAttnArgs& a, const SeqSpan& s) {
-    return static_cast<int>((static_cast<int64_t>(s.n) * a.rep + kPrTiles * kPrRows - 1) / (kPrTiles * kPrRows));
+// Pairs of row tiles of a sequence.
+__device__ __forceinline__ int pr_pairs(const PagedPromptArgs& g, const SeqSpan& s) {
+    constexpr int R = kPrTiles * kPrRows;
+    return s.n > g.skip ? static_cast<int>((static_cast<int64_t>(s.n) * g.a.rep + R - 1) / R) : 0;
 }
+// A pair's work goes by the positions that its last row sees; pair i of a sequence: min(window and first positions, first + 1 +
+// (256 (i + 1) - 1) / rep).  The largest of a sequence, and how many of its n pairs have at least `least`.
+__device__ __forceinline__ int pr_seen_at_most(const PagedAttnArgs& a) {
+    return a.mask.window > 0 ? min(a.mask.window, 1 << 29) + min(a.mask.sinks, 1 << 29) : 0x7FFFFFFF;
+}
+__device__ __forceinline__ int pr_most(const PagedAttnArgs& a, const SeqSpan& s, int n) {
+    return n > 0 ? min(pr_seen_at_most(a), max(s.first + 1 + static_cast<int>((static_cast<int64_t>(n) * kPrTiles * kPrRows - 1) / a.rep), 1)) : 0;
+}
+__device__ __forceinline__ int pr_count(const PagedAttnArgs& a, const SeqSpan& s, int n, int least) {
+    if (pr_seen_at_most(a) < least) return 0;
+    constexpr int R = kPrTiles * kPrRows;
+    const int64_t need = static_cast<int64_t>(least) - 1 - s.first;  // (256 (i + 1) - 1) / rep >= need
+    const int64_t from = need <= 0 ? 0 : max((need * a.rep + 1 + R - 1) / R - 1, int64_t{0});
+    return static_cast<int>(max(n - from, int64_t{0}));
+}
+constexpr int kPrClasses = 4;  // pairs with more than 1/2, 1/4, 1/8 of the longest one's positions, and the others
 
 // Bits 0 .. n - 1 of a word (n <= 0: none, n >= 32: all).
 __device__ __forceinline__ uint32_t pr_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
@@ -96,7 +115,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
     __shared__ PrWork work;
-    __shared__ int warp_tiles[kPrThreads / 32];
+    __shared__ int warp_most[kPrThreads / 32], warp_pairs[kPrThreads / 32][kPrClasses];
     __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -105,48 +124,90 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- which rows: blocks go through the sequences' pairs of row tiles, kv heads side by side, later rows (with more
-    // positions) first within a sequence
+    // ---- which rows: blocks go through the pairs of row tiles in classes of falling length (a long one that begins last is what
+    // everybody waits for), in a class sequence by sequence, kv heads side by side
     const int pair = blockIdx.x / a.w.n_kv;
     if (tid == 0) work.b = -1;
-    {
-        const int n = a.w.n_seqs, per = (n + kPrThreads - 1) / kPrThreads;
-        int mine = 0;
-        for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) mine += pr_row_tiles(a, paged_span(a.w, i, blockIdx.x == 0));
-        int incl = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-            if (lane >= o) incl += up;
+    auto take = [&](const SeqSpan& s, int b, int i) {  // pair i of sequence b
+        PrWork w;
+        w.s = s;
+        w.b = b;
+        w.kv_head = blockIdx.x % a.w.n_kv;
+        w.row_base = i * kPrTiles * kPrRows;
+        const int rows = s.n * a.rep;
+        const int first = max(s.first + w.row_base / a.rep, 0);
+        // (both on a box's border; places that no row sees are masked)
+        w.low = paged_low(a.mask, first) & ~(args.box - 1);
+        w.few = min((paged_few(a.mask, w.low) + args.box - 1) & ~(args.box - 1), w.low);
+        for (int x = 0; x < kPrTiles; ++x) {
+            const int r0 = w.row_base + x * kPrRows, r1 = min(r0 + kPrRows, rows) - 1;
+            const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
+            w.tiles[x] = last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 0;
         }
-        if (lane == 31) warp_tiles[warp] = incl;
+        work = w;
+    };
+    if (a.w.n_seqs == 1) {
+        if (tid == 0) {
+            const SeqSpan s = paged_span(a.w, 0, blockIdx.x == 0);
+            const int t = pr_pairs(args, s);
+            if (pair < t) take(s, 0, t - 1 - pair);
+        }
+    } else {
+        const int n = a.w.n_seqs, per = (n + kPrThreads - 1) / kPrThreads, i0 = tid * per, i1 = min(n, i0 + per);
+        SeqSpan one = {};
+        int longest = 0;
+        for (int i = i0; i < i1; ++i) {
+            one = paged_span(a.w, i, blockIdx.x == 0);
+            longest = max(longest, pr_most(a, one, pr_pairs(args, one)));
+        }
+        longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+        if (lane == 0) warp_most[warp] = longest;
         __syncthreads();
-        int before = incl - mine;
-        for (int w = 0; w < warp; ++w) before += warp_tiles[w];
-        if (pair >= before && pair < before + mine) {
-            for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
-                const SeqSpan s = paged_span(a.w, i, false);
-                const int t = pr_row_tiles(a, s);
-                if (pair < before + t) {
-                    PrWork w;
-                    w.s = s;
-                    w.b = i;
-                    w.kv_head = blockIdx.x % a.w.n_kv;
-                    w.row_base = (t - 1 - (pair - before)) * kPrTiles * kPrRows;
-                    const int rows = s.n * a.rep;
-                    const int first = max(s.first + w.row_base / a.rep, 0);
-                    // (both on a box's border; places that no row sees are masked)
-                    w.low = paged_low(a.mask, first) & ~(args.box - 1);
-                    w.few = min((paged_few(a.mask, w.low) + args.box - 1) & ~(args.box - 1), w.low);
-                    for (int x = 0; x < kPrTiles; ++x) {
-                        const int r0 = w.row_base + x * kPrRows, r1 = min(r0 + kPrRows, rows) - 1;
-                        const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
-                        w.tiles[x] = last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 0;
-                    }
-                    work = w;
+#pragma unroll
+        for (int x = 0; x < kPrThreads / 32; ++x) longest = max(longest, warp_most[x]);
+        int mine[kPrClasses] = {0, 0, 0, 0}, incl[kPrClasses];
+        for (int i = i0; i < i1; ++i) {
+            const SeqSpan s = per == 1 ? one : paged_span(a.w, i, false);
+            const int t = pr_pairs(args, s);
+            int up = 0;
+#pragma unroll
+            for (int c = 0; c < kPrClasses; ++c) {
+                const int upto = c + 1 < kPrClasses ? pr_count(a, s, t, (longest >> (c + 1)) + 1) : t;
+                mine[c] += upto - up;
+                up = upto;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kPrClasses; ++c) {
+            incl[c] = mine[c];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xFFFFFFFFu, incl[c], o);
+                if (lane >= o) incl[c] += up;
+            }
+            if (lane == 31) warp_pairs[warp][c] = incl[c];
+        }
+        __syncthreads();
+        int before = 0;  // pairs in front of this thread's of class c
+#pragma unroll
+        for (int c = 0; c < kPrClasses; ++c) {
+            int all = 0, at = before + incl[c] - mine[c];
+            for (int x = 0; x < kPrThreads / 32; ++x) {
+                if (x < warp) at += warp_pairs[x][c];
+                all += warp_pairs[x][c];
+            }
+            before += all;
+            if (pair < at || pair >= at + mine[c]) continue;
+            for (int i = i0; i < i1; ++i) {
+                const SeqSpan s = per == 1 ? one : paged_span(a.w, i, false);
+                const int t = pr_pairs(args, s);
+                const int up = c > 0 ? pr_count(a, s, t, (longest >> c) + 1) : 0;
+                const int upto = c + 1 < kPrClasses ? pr_count(a, s, t, (longest >> (c + 1)) + 1) : t;
+                if (pair - at < upto - up) {
+                    take(s, i, t - 1 - (up + pair - at));
                     break;
                 }
-                before += t;
+                at += upto - up;
             }
         }
     }
