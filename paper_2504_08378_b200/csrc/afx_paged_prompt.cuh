@@ -12,7 +12,9 @@
 // below 2^8; fp16 P is carried times 2^7, so that what is lost below its range is 2^-32 of the largest weight).
 // P is rounded to the cache's type (half a step of 2^-9 / 2^-12 relative per weight, averaged over the weights; the sums
 // of weights are taken before that rounding): 16-bit operands are what the tensor cores multiply at full rate.
-// Three warps fetch keys and values.  Pages of a multiple of 16 positions are read in boxes of 16 to 128 positions (the
+// A block stays: while the rows of a work leave, the loads and the first scores of the next one are under way.  It takes works over from
+// blocks of the grid that have not begun (cluster launch control), longest first.
+// Three warps fetch queries, keys and values.  Pages of a multiple of 16 positions are read in boxes of 16 to 128 positions (the
 // largest power of two that divides the page size) with tensor copies; other pages, and the tile in which the sequence
 // ends (what lies behind it in its page may be anything, and has to become zero), row by row with cp.async.  (Everything with
 // cp.async: the tensor cores waited 1300 of 4000 cycles per step for the copies.)
@@ -49,10 +51,10 @@ struct PrCfg {
 };
 
 struct PrBarriers {
-    uint64_t q_full, full[8], empty[8], s_full[2], p_half[2], p_full[2], o_full[2], drain;
+    uint64_t q_full, q_empty, full[8], empty[8], s_full[2], p_half[2], p_full[2], o_full[2], work_full[2], work_empty[2], answered, drain;
 };
 
-// What a block works on.
+// A work: what a block does at a time.
 struct PrWork {
     SeqSpan s;
     int b, kv_head, row_base;  // first of its 256 rows
@@ -103,36 +105,17 @@ __device__ __forceinline__ uint32_t pr_weights(float s0, float s1, f32x2 scale, 
     return pack2_bits<CT>(p0, p1);
 }
 
-template <int D, int CT>
-__global__ void __launch_bounds__(kPrThreads, 1)
-paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+// Work `place` of the grid: (pair of row tiles, kv head), kv heads side by side; the pairs in classes of falling length (a long one
+// that begins last is what everybody waits for), in a class sequence by sequence.  One warp; what it finds goes to
+// *out, nothing when there are not so many.  longest: -1 on the warp's first call.
+__device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, int& longest, PrWork* out) {
     const PagedAttnArgs& a = args.a;
-    using Cfg = PrCfg<D>;
-    constexpr int NB = Cfg::kRing;
-    constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
-    extern __shared__ unsigned char dyn_raw[];
-    __shared__ PrBarriers bar;
-    __shared__ uint32_t tmem_at;
-    __shared__ int gave_up;
-    __shared__ PrWork work;
-    __shared__ int warp_most[kPrThreads / 32], warp_pairs[kPrThreads / 32][kPrClasses];
-    __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const uint32_t base = smem_u32(dyn);
-
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-    // ---- which rows: blocks go through the pairs of row tiles in classes of falling length (a long one that begins last is what
-    // everybody waits for), in a class sequence by sequence, kv heads side by side
-    const int pair = blockIdx.x / a.w.n_kv;
-    if (tid == 0) work.b = -1;
+    const int pair = place / a.w.n_kv, lane = lane_id();
     auto take = [&](const SeqSpan& s, int b, int i) {  // pair i of sequence b
         PrWork w;
         w.s = s;
         w.b = b;
-        w.kv_head = blockIdx.x % a.w.n_kv;
+        w.kv_head = place - pair * a.w.n_kv;
         w.row_base = i * kPrTiles * kPrRows;
         const int rows = s.n * a.rep;
         const int first = max(s.first + w.row_base / a.rep, 0);
@@ -144,76 +127,85 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
             w.tiles[x] = last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 0;
         }
-        work = w;
+        *out = w;
     };
+    const bool first_call = longest < 0, report = first_call && blockIdx.x == 0;
     if (a.w.n_seqs == 1) {
-        if (tid == 0) {
-            const SeqSpan s = paged_span(a.w, 0, blockIdx.x == 0);
+        longest = 0;
+        if (lane == 0) {
+            const SeqSpan s = paged_span(a.w, 0, report);
             const int t = pr_pairs(args, s);
             if (pair < t) take(s, 0, t - 1 - pair);
         }
-    } else {
-        const int n = a.w.n_seqs, per = (n + kPrThreads - 1) / kPrThreads, i0 = tid * per, i1 = min(n, i0 + per);
-        SeqSpan one = {};
-        int longest = 0;
+        return;
+    }
+    const int n = a.w.n_seqs, per = (n + 31) / 32, i0 = lane * per, i1 = min(n, i0 + per);
+    if (first_call) {
+        longest = 0;
         for (int i = i0; i < i1; ++i) {
-            one = paged_span(a.w, i, blockIdx.x == 0);
-            longest = max(longest, pr_most(a, one, pr_pairs(args, one)));
+            const SeqSpan s = paged_span(a.w, i, report);
+            longest = max(longest, pr_most(a, s, pr_pairs(args, s)));
         }
         longest = __reduce_max_sync(0xFFFFFFFFu, longest);
-        if (lane == 0) warp_most[warp] = longest;
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < kPrThreads / 32; ++x) longest = max(longest, warp_most[x]);
-        int mine[kPrClasses] = {0, 0, 0, 0}, incl[kPrClasses];
+    }
+    int before = 0;  // pairs of the classes in front
+    for (int c = 0; c < kPrClasses; ++c) {
+        const int most = (longest >> c) + 1, least = (longest >> (c + 1)) + 1;
+        auto in_class = [&](const SeqSpan& s, int t, int& up) {
+            up = c > 0 ? pr_count(a, s, t, most) : 0;
+            return (c + 1 < kPrClasses ? pr_count(a, s, t, least) : t) - up;
+        };
+        int mine = 0, up;
         for (int i = i0; i < i1; ++i) {
-            const SeqSpan s = per == 1 ? one : paged_span(a.w, i, false);
-            const int t = pr_pairs(args, s);
-            int up = 0;
-#pragma unroll
-            for (int c = 0; c < kPrClasses; ++c) {
-                const int upto = c + 1 < kPrClasses ? pr_count(a, s, t, (longest >> (c + 1)) + 1) : t;
-                mine[c] += upto - up;
-                up = upto;
-            }
+            const SeqSpan s = paged_span(a.w, i, false);
+            mine += in_class(s, pr_pairs(args, s), up);
         }
+        int incl = mine;
 #pragma unroll
-        for (int c = 0; c < kPrClasses; ++c) {
-            incl[c] = mine[c];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int up = __shfl_up_sync(0xFFFFFFFFu, incl[c], o);
-                if (lane >= o) incl[c] += up;
-            }
-            if (lane == 31) warp_pairs[warp][c] = incl[c];
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += t;
         }
-        __syncthreads();
-        int before = 0;  // pairs in front of this thread's of class c
-#pragma unroll
-        for (int c = 0; c < kPrClasses; ++c) {
-            int all = 0, at = before + incl[c] - mine[c];
-            for (int x = 0; x < kPrThreads / 32; ++x) {
-                if (x < warp) at += warp_pairs[x][c];
-                all += warp_pairs[x][c];
-            }
-            before += all;
-            if (pair < at || pair >= at + mine[c]) continue;
+        const int all = __shfl_sync(0xFFFFFFFFu, incl, 31);
+        int at = before + incl - mine;
+        if (pair >= at && pair < at + mine) {
             for (int i = i0; i < i1; ++i) {
-                const SeqSpan s = per == 1 ? one : paged_span(a.w, i, false);
-                const int t = pr_pairs(args, s);
-                const int up = c > 0 ? pr_count(a, s, t, (longest >> c) + 1) : 0;
-                const int upto = c + 1 < kPrClasses ? pr_count(a, s, t, (longest >> (c + 1)) + 1) : t;
-                if (pair - at < upto - up) {
+                const SeqSpan s = paged_span(a.w, i, false);
+                const int t = pr_pairs(args, s), k = in_class(s, t, up);
+                if (pair - at < k) {
                     take(s, i, t - 1 - (up + pair - at));
                     break;
                 }
-                at += upto - up;
+                at += k;
             }
         }
+        before += all;
+        if (pair < before) break;
     }
+}
+
+template <int D, int CT>
+__global__ void __launch_bounds__(kPrThreads, 1)
+paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    const PagedAttnArgs& a = args.a;
+    using Cfg = PrCfg<D>;
+    constexpr int NB = Cfg::kRing;
+    constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
+    extern __shared__ unsigned char dyn_raw[];
+    __shared__ PrBarriers bar;
+    __shared__ __align__(16) uint4 answer;  // of the request for the next block
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    __shared__ PrWork work[2];
+    __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t base = smem_u32(dyn);
+
     if (tid == 0) {
         gave_up = 0;
-        mbar_init(&bar.q_full, kPrTiles * kPrRows);
+        mbar_init(&bar.q_full, kPrLoaders * 32);
+        mbar_init(&bar.q_empty, 1);
         for (int i = 0; i < NB; ++i) {
             mbar_init(&bar.full[i], kPrLoaders * 32);
             mbar_init(&bar.empty[i], 1);
@@ -223,67 +215,87 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             mbar_init(&bar.p_half[i], 4);
             mbar_init(&bar.p_full[i], 4);
             mbar_init(&bar.o_full[i], 1);
+            mbar_init(&bar.work_full[i], 1);
+            mbar_init(&bar.work_empty[i], kPrThreads / 32);
         }
+        mbar_init(&bar.answered, 1);
         mbar_init(&bar.drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
-    if (work.b < 0) return;  // (the grid is an upper bound; the same for all threads)
     if (warp == 8) tmem_alloc(&tmem_at, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    const PrWork w = work;
-    const int n_tiles = max(w.tiles[0], w.tiles[1]);
-    const int rows = w.s.n * a.rep;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // A warp's next work (in its registers), the same for the whole warp; b < 0: there is none.  it counts the block's works.
+    auto next_work = [&](int it, PrWork& w) {
+        const bool in = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.work_full[it & 1], (it >> 1) & 1, &gave_up));
+        if (in) {
+            w = work[it & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.work_empty[it & 1]);
+        }
+        return in;
+    };
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 8) {
             // ---- products: the warp goes through the waits together and one lane issues, so that the operands'
             // places stay in uniform registers (all of it in a lane's branch: 64 products took 3800 cycles of the thread's time)
-            if (n_tiles > 0) {
-                constexpr uint32_t s_desc = mma_desc(CT == AFX_BF16, 128, kPrPos, false);
-                constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
-                const bool lead = elect_one();
-                const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-                const int nt = __shfl_sync(0xFFFFFFFFu, n_tiles, 0);
-                const int tiles[2] = {__shfl_sync(0xFFFFFFFFu, w.tiles[0], 0), __shfl_sync(0xFFFFFFFFu, w.tiles[1], 0)};
-                auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
-                // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies are writes like any thread's, the
-                // products read shared memory by another path: the fence stands between what the barrier says and them.
-                int slot = 0;
-                uint32_t turn = 0;
-                auto arrived = [&]() {
-                    const bool in = wait(&bar.full[slot], turn);
-                    fence_proxy_async();
-                    return in;
-                };
-                auto step = [&]() {
-                    if (++slot == NB) {
-                        slot = 0;
-                        turn ^= 1u;
-                    }
-                };
-                auto scores = [&](int x, uint32_t k) {
-                    if (lead) {
-                        const uint32_t qd = smem_desc(base + Cfg::kQ + x * Cfg::kTile, 16), kd = smem_desc(base + Cfg::kKV + k * Cfg::kTile, 16);
+            constexpr uint32_t s_desc = mma_desc(CT == AFX_BF16, 128, kPrPos, false);
+            constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
+            const bool lead = elect_one();
+            const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
+            // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies are writes like any thread's, the
+            // products read shared memory by another path: the fence stands between what the barrier says and them.
+            int slot = 0;
+            uint32_t turn = 0, q_turn = 0, p_turn[2] = {0, 0};
+            auto arrived = [&]() {
+                const bool in = wait(&bar.full[slot], turn);
+                fence_proxy_async();
+                return in;
+            };
+            auto step = [&]() {
+                if (++slot == NB) {
+                    slot = 0;
+                    turn ^= 1u;
+                }
+            };
+            auto scores = [&](int x, uint32_t k) {
+                if (lead) {
+                    const uint32_t qd = smem_desc(base + Cfg::kQ + x * Cfg::kTile, 16), kd = smem_desc(base + Cfg::kKV + k * Cfg::kTile, 16);
 #pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            const uint32_t off = ((i / 4) * Cfg::kBlock + (i % 4) * 32) >> 4;
-                            tc_mma_ss(tm + x * kPrPos, qd + off, kd + off, s_desc, i > 0);
-                        }
-                        tc_commit(&bar.s_full[x]);
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = ((i / 4) * Cfg::kBlock + (i % 4) * 32) >> 4;
+                        tc_mma_ss(tm + x * kPrPos, qd + off, kd + off, s_desc, i > 0);
                     }
-                    __syncwarp();
-                };
-                bool ok = wait(&bar.q_full, 0) && arrived();
+                    tc_commit(&bar.s_full[x]);
+                }
+                __syncwarp();
+            };
+            bool ok = true;
+            for (int it = 0; ok; ++it) {
+                PrWork w;
+                ok = next_work(it, w);
+                if (!ok || w.b < 0) break;
+                const int tiles[2] = {__shfl_sync(0xFFFFFFFFu, w.tiles[0], 0), __shfl_sync(0xFFFFFFFFu, w.tiles[1], 0)};
+                const int nt = max(tiles[0], tiles[1]);
+                if (nt == 0) continue;
+                ok = wait(&bar.q_full, q_turn) && arrived();
+                q_turn ^= 1u;
                 if (ok) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x)
-                        if (tiles[x] > 0) scores(x, 0);
-                    if (lead) tc_commit(&bar.empty[0]);
+                        if (tiles[x] > 0) scores(x, slot);
+                    if (lead) {
+                        tc_commit(&bar.empty[slot]);
+                        if (nt == 1) tc_commit(&bar.q_empty);
+                    }
                     __syncwarp();
                     step();
                 }
@@ -304,7 +316,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                         const uint32_t vd = smem_desc(base + Cfg::kKV + vs * Cfg::kTile, Cfg::kBlock);
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            ok = ok && wait(half == 0 ? &bar.p_half[x] : &bar.p_full[x], j & 1);
+                            ok = ok && wait(half == 0 ? &bar.p_half[x] : &bar.p_full[x], p_turn[x]);
                             tc_fence_after();
                             if (ok && lead) {
 #pragma unroll
@@ -313,6 +325,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                             }
                             __syncwarp();
                         }
+                        p_turn[x] ^= 1u;
                         if (!ok) continue;
                         if (j + 1 < tiles[x]) {
                             scores(x, ks);
@@ -324,15 +337,16 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     if (ok && lead) {
                         tc_commit(&bar.empty[vs]);
                         if (j + 1 < nt) tc_commit(&bar.empty[ks]);
+                        if (j + 2 == nt) tc_commit(&bar.q_empty);  // the last scores of this work are issued
                     }
                     __syncwarp();
                 }
-                if (!ok && lead) {  // what has been issued ends before tensor memory is given back
-                    int alone = 0;
-                    report_status(a.w.status, AFX_ERR_TIMEOUT);
-                    tc_commit(&bar.drain);
-                    mbar_wait(&bar.drain, 0, &alone);
-                }
+            }
+            if (!ok && lead) {  // what has been issued ends before tensor memory is given back
+                int alone = 0;
+                report_status(a.w.status, AFX_ERR_TIMEOUT);
+                tc_commit(&bar.drain);
+                mbar_wait(&bar.drain, 0, &alone);
             }
             __syncwarp();
         } else {
@@ -346,232 +360,305 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             auto when_landed = [&](uint64_t* full) {  // an arrival of this thread's as soon as its copies so far have landed
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
             };
-            const int end = min(w.s.len, w.s.first + w.s.n);
-            int64_t off[3], next[3];
-            auto look_up = [&](int j) {
-#pragma unroll
-                for (int x = 0; x < 3; ++x) {
-                    const int v = j * kPrPos + (lw + x * kPrLoaders) * 16 + (lane & 15);
-                    const int p = v < w.few ? v : v - w.few + w.low;
-                    next[x] = -1;
-                    if (lw + x * kPrLoaders < 8 && p < end) {
-                        next[x] = paged_row(a.w, w.b, p, w.kv_head);
-                        if (next[x] < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
-                    }
-                }
-            };
-            // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).
+            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
             const int boxes = kPrPos / args.box;
-            // first tile that is not: it holds the sequence's end or (box = 1) any
-            const int n_boxed = args.box == 1 ? 0 : w.few + end - w.low >= 0 ? (w.few + end - w.low) / kPrPos : 0;
-            int page = -1, in_page = 0;
-            auto look_up_box = [&](int j) {
-                const int v = j * kPrPos + (lane % boxes) * args.box, p = v < w.few ? v : v - w.few + w.low;
-                page = paged_page(a.w, w.b, p, in_page);
-                if (page < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
-            };
-            auto fill_boxes = [&](const CUtensorMap* map, int n) {
-                const uint32_t tile = base + Cfg::kKV + (n % NB) * Cfg::kTile;
-                if (lane == 0) mbar_expect(&bar.full[n % NB], Cfg::kTile);
-                __syncwarp();
-                for (int x = lane; x < boxes * (D / 64); x += 32) {  // (boxes divides 32 or x stays below 32: the lane's own box)
-                    const int half = x / boxes, i = x % boxes;
-                    // a page that is none: out of the tensor, zeros
-                    tma_load_4d(tile + half * Cfg::kBlock + i * args.box * 128, map, half * 64, in_page, w.kv_head, page < 0 ? a.w.n_pages : page,
-                                &bar.full[n % NB]);
+            // the ring's next slot: its tile before has been used (after the first turn)
+            int slot = 0, ok_slot = 0;
+            uint32_t turn = 0, q_turn = 0;
+            bool q_used = false, ok = true;
+            int asked = 0;  // requests made, 0: none is open
+            auto room = [&]() { return turn == 0 || wait(&bar.empty[slot], (turn & 1u) ^ 1u); };
+            auto step = [&]() {
+                if (++slot == NB) {
+                    slot = 0;
+                    ++turn;
                 }
-                if (lane != 0) mbar_arrive(&bar.full[n % NB]);
             };
-            auto fill = [&](const uint16_t* pages, int n) {
-                const uint32_t tile = base + Cfg::kKV + (n % NB) * Cfg::kTile;
-#pragma unroll
-                for (int x = 0; x < 3; ++x) {
-                    const int blk = lw + x * kPrLoaders;
-                    if (blk >= 8) continue;
-#pragma unroll
-                    for (int i = 0; i < 16 / RPI; ++i) {
-                        const int row = i * RPI + lane / PIECES, piece = lane % PIECES;
-                        const int64_t o = __shfl_sync(0xFFFFFFFFu, off[x], row);
-                        put(tile, blk * 16 + row, piece, pages + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+            int longest = -1;
+            for (int it = 0; ok; ++it) {
+                if (lw == 2) {
+                    // ---- this warp finds the block's works: the first by its place in the grid, the others by taking over
+                    // places whose blocks have not begun (where that is refused they begin as blocks of their own)
+                    int place = blockIdx.x;
+                    if (it > 0) {
+                        ok = wait(&bar.answered, (it - 1) & 1);
+                        asked = 0;
+                        place = ok ? clc_place(&answer) : -1;
+                        fence_proxy_async();
                     }
+                    if (it >= 2 && ok) ok = wait(&bar.work_empty[it & 1], ((it >> 1) & 1) ^ 1);
+                    if (ok) {
+                        if (lane == 0) work[it & 1].b = -1;
+                        __syncwarp();
+                        if (place >= 0) pr_find(args, place, longest, &work[it & 1]);
+                        __syncwarp();
+                        const bool some = work[it & 1].b >= 0;
+                        if (lane == 0) mbar_arrive(&bar.work_full[it & 1]);
+                        if (some) {  // (places behind the last work are the end)
+                            asked = it + 1;
+                            if (lane == 0) {
+                                mbar_expect(&bar.answered, 16);
+                                clc_ask(&answer, &bar.answered);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
                 }
-                when_landed(&bar.full[n % NB]);
-            };
-            auto room = [&](int n) {  // tile n - NB of the ring has been used
-                return n < NB || __all_sync(0xFFFFFFFFu, mbar_wait(&bar.empty[n % NB], ((n / NB) & 1) ^ 1, &gave_up));
-            };
-            bool ok = true;
-            if (lw < n_boxed) look_up_box(lw);
-            if (n_boxed == 0) look_up(0);
-            for (int j = 0; j < n_tiles; ++j) {
-                const bool boxed = j < n_boxed, mine = boxed && j % kPrLoaders == lw;
-                if (!boxed) {
-#pragma unroll
-                    for (int x = 0; x < 3; ++x) off[x] = next[x];
-                }
-                if (j + 1 < n_tiles && j + 1 >= n_boxed) look_up(j + 1);
-                ok = room(2 * j);
-                if (!ok) break;
-                if (!boxed) {
+                PrWork w;
+                ok = next_work(it, w);
+                if (!ok || w.b < 0) break;
+                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.s.n * a.rep;
+                if (n_tiles == 0) continue;
+                const int end = min(w.s.len, w.s.first + w.s.n);
+                int64_t off[3], next[3];
+                auto look_up = [&](int j) {
 #pragma unroll
                     for (int x = 0; x < 3; ++x) {
-                        const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
-                        if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[j & 7][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                        const int v = j * kPrPos + (lw + x * kPrLoaders) * 16 + (lane & 15);
+                        const int p = v < w.few ? v : v - w.few + w.low;
+                        next[x] = -1;
+                        if (lw + x * kPrLoaders < 8 && p < end) {
+                            next[x] = paged_row(a.w, w.b, p, w.kv_head);
+                            if (next[x] < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
+                        }
                     }
-                    fill(a.w.k, 2 * j);
-                } else if (mine) {
-                    const uint32_t m = __ballot_sync(0xFFFFFFFFu, page >= 0);
-                    if (lane < 8) page_ok[j & 7][lane] = (m >> (lane * 16 / args.box)) & 1u ? 0xFFFFu : 0u;
-                    fill_boxes(&k_map, 2 * j);
-                } else {
-                    mbar_arrive(&bar.full[2 * j % NB]);
-                }
-                ok = room(2 * j + 1);
-                if (!ok) break;
-                if (!boxed) {
-                    fill(a.w.v, 2 * j + 1);
-                } else if (mine) {
-                    fill_boxes(&v_map, 2 * j + 1);
-                    if (j + kPrLoaders < n_boxed) look_up_box(j + kPrLoaders);
-                } else {
-                    mbar_arrive(&bar.full[(2 * j + 1) % NB]);
+                };
+                auto fill = [&](const uint16_t* pages) {
+                    const uint32_t tile = base + Cfg::kKV + slot * Cfg::kTile;
+#pragma unroll
+                    for (int x = 0; x < 3; ++x) {
+                        const int blk = lw + x * kPrLoaders;
+                        if (blk >= 8) continue;
+#pragma unroll
+                        for (int i = 0; i < 16 / RPI; ++i) {
+                            const int row = i * RPI + lane / PIECES, piece = lane % PIECES;
+                            const int64_t o = __shfl_sync(0xFFFFFFFFu, off[x], row);
+                            put(tile, blk * 16 + row, piece, pages + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+                        }
+                    }
+                    when_landed(&bar.full[slot]);
+                };
+                // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).  The first that is not
+                // holds the sequence's end, or (box = 1) any.
+                const int n_boxed = args.box == 1 || w.few + end < w.low ? 0 : (w.few + end - w.low) / kPrPos;
+                int page = -1, in_page = 0;
+                auto look_up_box = [&](int j) {
+                    const int v = j * kPrPos + (lane % boxes) * args.box, p = v < w.few ? v : v - w.few + w.low;
+                    page = paged_page(a.w, w.b, p, in_page);
+                    if (page < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
+                };
+                auto fill_boxes = [&](const CUtensorMap* map) {
+                    const uint32_t tile = base + Cfg::kKV + slot * Cfg::kTile;
+                    if (lane == 0) mbar_expect(&bar.full[slot], Cfg::kTile);
+                    __syncwarp();
+                    if (lane < boxes * (D / 64)) {
+                        const int half = lane / boxes, i = lane % boxes;
+                        // a page that is none: out of the tensor, zeros
+                        tma_load_4d(tile + half * Cfg::kBlock + i * args.box * 128, map, half * 64, in_page, w.kv_head, page < 0 ? a.w.n_pages : page,
+                                    &bar.full[slot]);
+                    }
+                    if (lane != 0) mbar_arrive(&bar.full[slot]);
+                };
+                if (lw < n_boxed) look_up_box(lw);
+                if (n_boxed == 0) look_up(0);
+                for (int j = 0; j < n_tiles; ++j) {
+                    const bool boxed = j < n_boxed, mine = boxed && j % kPrLoaders == lw;
+                    if (!boxed) {
+#pragma unroll
+                        for (int x = 0; x < 3; ++x) off[x] = next[x];
+                    }
+                    if (j + 1 < n_tiles && j + 1 >= n_boxed) look_up(j + 1);
+                    ok = room();
+                    if (!ok) break;
+                    if (!boxed) {
+#pragma unroll
+                        for (int x = 0; x < 3; ++x) {
+                            const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
+                            if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[ok_slot][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                        }
+                        fill(a.w.k);
+                    } else if (mine) {
+                        const uint32_t m = __ballot_sync(0xFFFFFFFFu, page >= 0);
+                        if (lane < 8) page_ok[ok_slot][lane] = (m >> (lane * 16 / args.box)) & 1u ? 0xFFFFu : 0u;
+                        fill_boxes(&k_map);
+                    } else {
+                        mbar_arrive(&bar.full[slot]);
+                    }
+                    ok_slot = (ok_slot + 1) & 7;
+                    step();
+                    if (j == 0) {
+                        // the 256 query rows, 32 to a turn of the warp; the work before has made its last scores
+                        if (q_used) {
+                            ok = wait(&bar.q_empty, q_turn);
+                            q_turn ^= 1u;
+                            if (!ok) break;
+                        }
+                        q_used = true;
+                        for (int blk = lw; blk < kPrTiles * kPrRows / 32; blk += kPrLoaders) {
+                            const int rr = w.row_base + blk * 32 + lane, i = rr / a.rep;
+                            const int64_t from = rr < rows ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D : -1;
+#pragma unroll
+                            for (int k = 0; k < 32 / RPI; ++k) {
+                                const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
+                                const int64_t o = __shfl_sync(0xFFFFFFFFu, from, row);
+                                put(base + Cfg::kQ + (blk / 4) * Cfg::kTile, (blk % 4) * 32 + row, piece,
+                                    reinterpret_cast<const uint16_t*>(a.q) + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+                            }
+                        }
+                        when_landed(&bar.q_full);
+                    }
+                    ok = room();
+                    if (!ok) break;
+                    if (!boxed) {
+                        fill(a.w.v);
+                    } else if (mine) {
+                        fill_boxes(&v_map);
+                        if (j + kPrLoaders < n_boxed) look_up_box(j + kPrLoaders);
+                    } else {
+                        mbar_arrive(&bar.full[slot]);
+                    }
+                    step();
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
+            if (!ok) {
+                if (lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
+                if (asked > 0) {  // the answer is written before the block ends
+                    int alone = 0;
+                    mbar_wait(&bar.answered, (asked - 1) & 1, &alone);
+                }
+            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ---- softmax: a thread per row
-        const int x = warp >> 2, r = (warp & 3) * 32 + lane, rr = w.row_base + x * kPrRows + r;
+        const int x = warp >> 2;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + x * kPrPos, o_at = tmem + lanes + 256 + x * D;
-        const int i = rr / a.rep, h = w.kv_head * a.rep + rr - i * a.rep;
-        const bool live = rr < rows;
-        const int pos = live ? w.s.first + i : -1;
-        const int shift = w.few - w.low;  // place in the list of visible positions = position + shift, behind the first ones
-        const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
-        const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
-        const int v_few = a.mask.window > 0 ? a.mask.sinks : 0;  // (first positions are their own places: few covers them, or few = low)
-        {  // the warp's 32 query rows into shared memory, 16 (or 8) lanes to a row
-            constexpr int PIECES = D / 8, RPI = 32 / PIECES;
-            const int64_t from = live ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(h) * D : -1;
-            const uint32_t tile = base + Cfg::kQ + x * Cfg::kTile;
-#pragma unroll
-            for (int k = 0; k < 32 / RPI; ++k) {
-                const int row = k * RPI + lane / PIECES, piece = lane % PIECES, tr = (warp & 3) * 32 + row;
-                const int64_t o = __shfl_sync(0xFFFFFFFFu, from, row);
-                const uint32_t to = tile + (piece >> 3) * Cfg::kBlock + tr * 128 + (((piece & 7) ^ (tr & 7)) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to),
-                             "l"(reinterpret_cast<const uint16_t*>(a.q) + (o < 0 ? 0 : o) + piece * 8), "r"(o < 0 ? 0 : 16)
-                             : "memory");
-            }
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar.q_full)) : "memory");
-        }
-        // places that every row of the tile sees: below v_few and [lo_all, hi_all]
-        const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
-        const int hi_all = w.s.first + rr0 / a.rep + shift;
-        const int lo_all = a.mask.window > 0 ? w.s.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
         const float scale = fabsf(a.scale);
-        float m = -INFINITY, l = 0.0f;
+        uint32_t s_turn = 0, o_turn = 0;
+        int ok_slot = 0;
         bool ok = true;
-        for (int j = 0; ok && j < w.tiles[x]; ++j) {
-            ok = mbar_wait(&bar.s_full[x], j & 1, &gave_up);
-            if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-            tc_fence_after();
-            float s[kPrPos];
+        for (int it = 0; ok; ++it) {
+            PrWork w;
+            ok = next_work(it, w);
+            if (!ok || w.b < 0) break;
+            const int rows = w.s.n * a.rep;
+            const int rr = w.row_base + x * kPrRows + (warp & 3) * 32 + lane;
+            const int i = rr / a.rep, h = w.kv_head * a.rep + rr - i * a.rep;
+            const bool live = rr < rows;
+            const int pos = live ? w.s.first + i : -1;
+            const int shift = w.few - w.low;  // place in the list of visible positions = position + shift, behind the first ones
+            const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
+            const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
+            const int v_few = a.mask.window > 0 ? a.mask.sinks : 0;  // (first positions are their own places: few covers them, or few = low)
+            // places that every row of the tile sees: below v_few and [lo_all, hi_all]
+            const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
+            const int hi_all = w.s.first + rr0 / a.rep + shift;
+            const int lo_all = a.mask.window > 0 ? w.s.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
+            float m = -INFINITY, l = 0.0f;
+            for (int j = 0; ok && j < w.tiles[x]; ++j) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.s_full[x], s_turn, &gave_up));
+                s_turn ^= 1u;
+                if (!ok) break;
+                tc_fence_after();
+                float s[kPrPos];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, s_at + 32 * c);
-            tmem_wait_ld();
-            if (a.scale < 0.0f) {  // the largest of s times a negative scale is that of the smallest s
+                for (int c = 0; c < 4; ++c) tmem_ld32(s + 32 * c, s_at + 32 * c);
+                tmem_wait_ld();
+                if (a.scale < 0.0f) {  // the largest of s times a negative scale is that of the smallest s
 #pragma unroll
-                for (int c = 0; c < kPrPos; ++c) s[c] = -s[c];
-            }
-            const int v0 = j * kPrPos;
-            const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[j & 7]);
-            const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
-            const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= v_few);
-            if (!all) {  // 32 places as bits: those up to v_hi that are from v_lo on or below v_few, and have a page
-                const uint32_t word[4] = {okw.x, okw.y, okw.z, okw.w};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int v = v0 + 32 * c;
-                    const uint32_t see = pr_below(v_hi + 1 - v) & (~pr_below(v_lo - v) | pr_below(v_few - v)) & word[c];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) s[32 * c + e] = (see & (1u << e)) != 0u ? s[32 * c + e] : -INFINITY;
+                    for (int c = 0; c < kPrPos; ++c) s[c] = -s[c];
                 }
-            }
-            if (j == 0) {  // the first maximum is the reference; afterwards it stays while it is not exceeded by far
-                float top = fmaxf(s[0], s[1]);
+                const int v0 = j * kPrPos;
+                const uint4 okw = *reinterpret_cast<const uint4*>(page_ok[(ok_slot + j) & 7]);
+                const bool pages = (okw.x & okw.y & okw.z & okw.w) == 0xFFFFFFFFu;
+                const bool all = pages && v0 + kPrPos - 1 <= hi_all && (v0 >= lo_all || v0 + kPrPos <= v_few);
+                if (!all) {  // 32 places as bits: those up to v_hi that are from v_lo on or below v_few, and have a page
+                    const uint32_t word[4] = {okw.x, okw.y, okw.z, okw.w};
 #pragma unroll
-                for (int c = 2; c < kPrPos; c += 2) top = max3(top, s[c], s[c + 1]);
-                m = top * scale;
-            }
-            const f32x2 scale2 = pack_f32x2(scale, scale);
-            uint32_t p[kPrPos / 4];
-            f32x2 sum[2];
-            // The first half of the weights and, beside them, the maximum of all scores; when a row's has grown by too much
-            // (seldom), the rows' sums so far are rescaled and the weights taken again.
-            for (int pass = 0; pass < 2; ++pass) {
-                const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
-                const f32x2 ref2 = pack_f32x2(-ref, -ref);
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                sum[0] = sum[1] = 0;
+                    for (int c = 0; c < 4; ++c) {
+                        const int v = v0 + 32 * c;
+                        const uint32_t see = pr_below(v_hi + 1 - v) & (~pr_below(v_lo - v) | pr_below(v_few - v)) & word[c];
 #pragma unroll
-                for (int e = 0; e < kPrPos / 4; ++e) {
-                    p[e] = pr_weights<CT>(s[2 * e], s[2 * e + 1], scale2, ref2, sum[e & 1]);
-                    mx[(2 * e) & 3] = max3(mx[(2 * e) & 3], s[4 * e], s[4 * e + 1]);
-                    mx[(2 * e + 1) & 3] = max3(mx[(2 * e + 1) & 3], s[4 * e + 2], s[4 * e + 3]);
-                }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
-                if (pass == 1 || !__any_sync(0xFFFFFFFFu, grow)) break;
-                const float f = grow ? fast_exp2(m - top) : 1.0f;  // 0 where nothing was seen before
-                if (grow) m = top;
-                l *= f;
-                if (j > 0) {  // (the scores are there: what was issued before them, O's last addition too, is done)
-#pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        float o[16];
-                        tmem_ld16(o, o_at + 16 * c);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] *= f;
-                        tmem_st16(o_at + 16 * c, reinterpret_cast<const uint32_t*>(o));
+                        for (int e = 0; e < 32; ++e) s[32 * c + e] = (see & (1u << e)) != 0u ? s[32 * c + e] : -INFINITY;
                     }
                 }
-            }
-            tmem_st16(s_at, p);
-            tmem_st16(s_at + 16, p + 16);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.p_half[x]);  // half of the positions may be multiplied
-            {
-                const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
-                const f32x2 ref2 = pack_f32x2(-ref, -ref);
+                if (j == 0) {  // the first maximum is the reference; afterwards it stays while it is not exceeded by far
+                    float top = fmaxf(s[0], s[1]);
 #pragma unroll
-                for (int e = 0; e < kPrPos / 4; ++e)
-                    p[e] = pr_weights<CT>(s[kPrPos / 2 + 2 * e], s[kPrPos / 2 + 2 * e + 1], scale2, ref2, sum[e & 1]);
+                    for (int c = 2; c < kPrPos; c += 2) top = max3(top, s[c], s[c + 1]);
+                    m = top * scale;
+                }
+                const f32x2 scale2 = pack_f32x2(scale, scale);
+                uint32_t p[kPrPos / 4];
+                f32x2 sum[2];
+                // The first half of the weights and, beside them, the maximum of all scores; when a row's has grown by too much
+                // (seldom), the rows' sums so far are rescaled and the weights taken again.
+                for (int pass = 0; pass < 2; ++pass) {
+                    const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
+                    const f32x2 ref2 = pack_f32x2(-ref, -ref);
+                    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    sum[0] = sum[1] = 0;
+#pragma unroll
+                    for (int e = 0; e < kPrPos / 4; ++e) {
+                        p[e] = pr_weights<CT>(s[2 * e], s[2 * e + 1], scale2, ref2, sum[e & 1]);
+                        mx[(2 * e) & 3] = max3(mx[(2 * e) & 3], s[4 * e], s[4 * e + 1]);
+                        mx[(2 * e + 1) & 3] = max3(mx[(2 * e + 1) & 3], s[4 * e + 2], s[4 * e + 3]);
+                    }
+                    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                    const bool grow = top > m + kPrGrow || (m == -INFINITY && top > m);
+                    if (pass == 1 || !__any_sync(0xFFFFFFFFu, grow)) break;
+                    const float f = grow ? fast_exp2(m - top) : 1.0f;  // 0 where nothing was seen before
+                    if (grow) m = top;
+                    l *= f;
+                    if (j > 0) {  // (the scores are there: what was issued before them, O's last addition too, is done)
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c) {
+                            float o[16];
+                            tmem_ld16(o, o_at + 16 * c);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] *= f;
+                            tmem_st16(o_at + 16 * c, reinterpret_cast<const uint32_t*>(o));
+                        }
+                    }
+                }
+                tmem_st16(s_at, p);
+                tmem_st16(s_at + 16, p + 16);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.p_half[x]);  // half of the positions may be multiplied
+                {
+                    const float ref = m == -INFINITY ? 0.0f : m - kUpLog;
+                    const f32x2 ref2 = pack_f32x2(-ref, -ref);
+#pragma unroll
+                    for (int e = 0; e < kPrPos / 4; ++e)
+                        p[e] = pr_weights<CT>(s[kPrPos / 2 + 2 * e], s[kPrPos / 2 + 2 * e + 1], scale2, ref2, sum[e & 1]);
+                }
+                tmem_st16(s_at + 32, p);
+                tmem_st16(s_at + 48, p + 16);
+                float sums[4];
+                unpack_f32x2(sum[0], sums[0], sums[1]);
+                unpack_f32x2(sum[1], sums[2], sums[3]);
+                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar.p_full[x]);
             }
-            tmem_st16(s_at + 32, p);
-            tmem_st16(s_at + 48, p + 16);
-            float sums[4];
-            unpack_f32x2(sum[0], sums[0], sums[1]);
-            unpack_f32x2(sum[1], sums[2], sums[3]);
-            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar.p_full[x]);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        if (ok && w.tiles[x] > 0) {
-            ok = mbar_wait(&bar.o_full[x], 0, &gave_up);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            tc_fence_after();
-        }
-        if (ok) {
+            if (!ok) break;
+            ok_slot = (ok_slot + max(w.tiles[0], w.tiles[1])) & 7;
+            if (w.tiles[x] > 0) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.o_full[x], o_turn, &gave_up));
+                o_turn ^= 1u;
+                if (!ok) break;
+                tc_fence_after();
+            }
+            // ---- the rows leave.  (Straight from the threads: staged in shared memory they would leave in whole lines, but the
+            // next work's queries are on their way into the room for that.)
             const int64_t at = static_cast<int64_t>(w.s.row0 + i) * a.heads + h;
             float o[D];
             if (w.tiles[x] > 0) {
@@ -590,36 +677,18 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 fin &= fabsf(o[c]) <= 3.402823466e38f;
                 o[c] = none ? 0.0f : o[c] * inv;
             }
-            {  // through the shared memory of the warp's queries, so that rows leave in whole lines
-                constexpr int PIECES = D / 8, RPI = 32 / PIECES;
-                const uint32_t mine = base + Cfg::kQ + x * Cfg::kTile + (warp & 3) * 32 * D * 2;
-                __syncwarp();
+            if (live && fin) {
+                uint4* dst = reinterpret_cast<uint4*>(a.out + at * D);
 #pragma unroll
-                for (int c = 0; c < PIECES; ++c) {
+                for (int c = 0; c < D / 8; ++c) {
                     const float* t = o + 8 * c;
-                    const uint4 y = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
-                                                                       pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
-                                                          : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
-                                                                       pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(mine + lane * (D * 2) + ((c ^ (lane & 7)) << 4)), "r"(y.x),
-                                 "r"(y.y), "r"(y.z), "r"(y.w)
-                                 : "memory");
+                    dst[c] = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
+                                                                pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
+                                                   : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
+                                                                pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
                 }
-                __syncwarp();
-                const uint32_t good = __ballot_sync(0xFFFFFFFFu, live && fin);
-#pragma unroll
-                for (int k = 0; k < 32 / RPI; ++k) {
-                    const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
-                    const int64_t to = __shfl_sync(0xFFFFFFFFu, at, row);
-                    uint4 y;
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
-                                 : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w)
-                                 : "r"(mine + row * (D * 2) + ((piece ^ (row & 7)) << 4))
-                                 : "memory");
-                    if ((good >> row) & 1u) reinterpret_cast<uint4*>(a.out + to * D)[piece] = y;
-                }
+                if (a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
             }
-            if (live && fin && a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
             // Rows whose sums are not finite: what they do not see may have been NaN or infinite (a weight of zero times it).
             // Again, over what the row sees alone, on the fp32 pipe.
             uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin);
@@ -646,11 +715,10 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     a.out[wat * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
                 if (a.lse != nullptr && lane == 0) a.lse[wat] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
             }
-        } else if (lane == 0) {
-            report_status(a.w.status, AFX_ERR_TIMEOUT);
         }
+        if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
     }
-    // ---- nothing is in flight any more: all products were waited for by the rows' threads, all copies by the loaders
+    // ---- nothing is in flight any more: all products were waited for by the rows' threads, all copies by the loaders or them
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

@@ -61,6 +61,34 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ---- cluster launch control
+
+// Asks to take over a block of this grid that has not begun; the 16-byte answer arrives with the barrier.
+__device__ __forceinline__ void clc_ask(uint4* answer, uint64_t* bar) {
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(answer)),
+                 "r"(smem_u32(bar))
+                 : "memory");
+}
+// The block's index in x; -1: refused, or there was none.
+__device__ __forceinline__ int clc_place(const uint4* answer) {
+    uint32_t taken, x;
+    uint64_t lo, hi;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(lo), "=l"(hi) : "r"(smem_u32(answer)) : "memory");
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        ".reg .b128 h;\n"
+        "mov.b128 h, {%2, %3};\n"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "mov.u32 %1, 0;\n"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n"
+        "}\n"
+        : "=&r"(taken), "=&r"(x)
+        : "l"(lo), "l"(hi));
+    return taken != 0 ? static_cast<int>(x) : -1;
+}
+
 // ---- tensor memory
 
 __device__ __forceinline__ void tmem_alloc(uint32_t* out, int columns) {  // one whole warp
