@@ -31,6 +31,9 @@ namespace afx {
 constexpr int kPrThreads = 384;  // warps 0-3: rows of tile 0, 4-7: tile 1, 8: products, 9-11: loads
 constexpr int kPrRows = 128, kPrTiles = 2, kPrPos = 128;
 constexpr int kPrLoaders = 3;
+// Registers of a thread of the loading and issuing warps, and of the rows' warps: 128 and 256 threads share the 384 x 168 of the launch.
+constexpr int kPrLoadRegs = 104, kPrRowRegs = 200;
+static_assert(128 * kPrLoadRegs + 256 * kPrRowRegs <= kPrThreads * 168, "more than the launch has");
 constexpr float kPrGrow = 8.0f;  // powers of two that a row's maximum may grow by before O is rescaled
 
 struct PagedPromptArgs {
@@ -125,7 +128,8 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         for (int x = 0; x < kPrTiles; ++x) {
             const int r0 = w.row_base + x * kPrRows, r1 = min(r0 + kPrRows, rows) - 1;
             const int last = r0 < rows ? s.first + r1 / a.rep : -1;  // position of the tile's last row
-            w.tiles[x] = last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 0;
+            // (rows in front of the sequence see nothing of their one tile)
+            w.tiles[x] = r0 >= rows ? 0 : last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 1;
         }
         *out = w;
     };
@@ -230,6 +234,17 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
+    // One warp of the loaders finds the block's works: the first by its place in the grid, the others by taking over places
+    // whose blocks have not begun (where that is refused they begin as blocks of their own).
+    int longest = -1;
+    if (warp == 11) {
+        if (lane == 0) work[0].b = -1;
+        __syncwarp();
+        pr_find(args, blockIdx.x, longest, &work[0]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar.work_full[0]);
+    }
+
     // A warp's next work (in its registers), the same for the whole warp; b < 0: there is none.  it counts the block's works.
     auto next_work = [&](int it, PrWork& w) {
         const bool in = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.work_full[it & 1], (it >> 1) & 1, &gave_up));
@@ -242,7 +257,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     };
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPrLoadRegs));
         if (warp == 8) {
             // ---- products: the warp goes through the waits together and one lane issues, so that the operands'
             // places stay in uniform registers (all of it in a lane's branch: 64 products took 3800 cycles of the thread's time)
@@ -285,7 +300,6 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 if (!ok || w.b < 0) break;
                 const int tiles[2] = {__shfl_sync(0xFFFFFFFFu, w.tiles[0], 0), __shfl_sync(0xFFFFFFFFu, w.tiles[1], 0)};
                 const int nt = max(tiles[0], tiles[1]);
-                if (nt == 0) continue;
                 ok = wait(&bar.q_full, q_turn) && arrived();
                 q_turn ^= 1u;
                 if (ok) {
@@ -374,42 +388,19 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     ++turn;
                 }
             };
-            int longest = -1;
             for (int it = 0; ok; ++it) {
-                if (lw == 2) {
-                    // ---- this warp finds the block's works: the first by its place in the grid, the others by taking over
-                    // places whose blocks have not begun (where that is refused they begin as blocks of their own)
-                    int place = blockIdx.x;
-                    if (it > 0) {
-                        ok = wait(&bar.answered, (it - 1) & 1);
-                        asked = 0;
-                        place = ok ? clc_place(&answer) : -1;
-                        fence_proxy_async();
-                    }
-                    if (it >= 2 && ok) ok = wait(&bar.work_empty[it & 1], ((it >> 1) & 1) ^ 1);
-                    if (ok) {
-                        if (lane == 0) work[it & 1].b = -1;
-                        __syncwarp();
-                        if (place >= 0) pr_find(args, place, longest, &work[it & 1]);
-                        __syncwarp();
-                        const bool some = work[it & 1].b >= 0;
-                        if (lane == 0) mbar_arrive(&bar.work_full[it & 1]);
-                        if (some) {  // (places behind the last work are the end)
-                            asked = it + 1;
-                            if (lane == 0) {
-                                mbar_expect(&bar.answered, 16);
-                                clc_ask(&answer, &bar.answered);
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    if (!ok) break;
-                }
                 PrWork w;
                 ok = next_work(it, w);
                 if (!ok || w.b < 0) break;
                 const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.s.n * a.rep;
-                if (n_tiles == 0) continue;
+                if (lw == 2) {  // a place in the grid whose block has not begun, if there is one
+                    asked = it + 1;
+                    if (lane == 0) {
+                        mbar_expect(&bar.answered, 16);
+                        clc_ask(&answer, &bar.answered);
+                    }
+                    __syncwarp();
+                }
                 const int end = min(w.s.len, w.s.first + w.s.n);
                 int64_t off[3], next[3];
                 auto look_up = [&](int j) {
@@ -519,6 +510,21 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                         mbar_arrive(&bar.full[slot]);
                     }
                     step();
+                    if (lw == 2 && j == min(2, n_tiles - 1)) {
+                        // the next work, as soon as this one's first tiles are on their way
+                        ok = wait(&bar.answered, it & 1);
+                        asked = 0;
+                        const int place = ok ? clc_place(&answer) : -1;
+                        fence_proxy_async();
+                        if (ok && it >= 1) ok = wait(&bar.work_empty[(it + 1) & 1], (((it + 1) >> 1) & 1) ^ 1);
+                        if (!ok) break;
+                        if (lane == 0) work[(it + 1) & 1].b = -1;
+                        __syncwarp();
+                        if (place >= 0) pr_find(args, place, longest, &work[(it + 1) & 1]);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&bar.work_full[(it + 1) & 1]);
+                        __syncwarp();
+                    }
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -531,7 +537,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPrRowRegs));
         // ---- softmax: a thread per row
         const int x = warp >> 2;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -678,14 +684,25 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 o[c] = none ? 0.0f : o[c] * inv;
             }
             if (live && fin) {
-                uint4* dst = reinterpret_cast<uint4*>(a.out + at * D);
+                uint16_t* dst = a.out + at * D;
+                uint32_t y[D / 2];
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) {
                     const float* t = o + 8 * c;
-                    dst[c] = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
+                    *reinterpret_cast<uint4*>(y + 4 * c) = a.out_type == AFX_F16 ? make_uint4(pack2_bits<AFX_F16>(t[0], t[1]), pack2_bits<AFX_F16>(t[2], t[3]),
                                                                 pack2_bits<AFX_F16>(t[4], t[5]), pack2_bits<AFX_F16>(t[6], t[7]))
                                                    : make_uint4(pack2_bits<AFX_BF16>(t[0], t[1]), pack2_bits<AFX_BF16>(t[2], t[3]),
                                                                 pack2_bits<AFX_BF16>(t[4], t[5]), pack2_bits<AFX_BF16>(t[6], t[7]));
+                }
+                if ((reinterpret_cast<uintptr_t>(a.out) & 31u) == 0) {  // whole sectors
+#pragma unroll
+                    for (int c = 0; c < D / 16; ++c)
+                        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst + 16 * c), "r"(y[8 * c]), "r"(y[8 * c + 1]),
+                                     "r"(y[8 * c + 2]), "r"(y[8 * c + 3]), "r"(y[8 * c + 4]), "r"(y[8 * c + 5]), "r"(y[8 * c + 6]), "r"(y[8 * c + 7])
+                                     : "memory");
+                } else {
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(dst)[c] = *reinterpret_cast<const uint4*>(y + 4 * c);
                 }
                 if (a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
             }
