@@ -19,8 +19,11 @@
 // ends (what lies behind it in its page may be anything, and has to become zero), row by row with cp.async.  (Everything with
 // cp.async: the tensor cores waited 1300 of 4000 cycles per step for the copies.)
 //
-// Bound by the exponentials and the products alike: 2 x 128 x 128 exponentials are 2048 cycles of an SM's 16 per cycle, the four products
-// 2048 cycles at D = 128.
+// A step of both row tiles takes 3600 cycles at D = 128 (8192 new tokens of 64 / 8 heads: 1.08 ms, 1020 TFLOP/s, 73 % of cuBLAS in a
+// loop under the power limit), where its 2 x 128 x 128 exponentials are 2048 cycles of the special-function units and
+// its products 2048 cycles of the tensor cores: a row tile's chain (scores, weights, products) is what is long, and the
+// two chains fill each other's gaps only in part.  Exponentials by polynomials on the fp32 pipe for an eighth or a quarter of
+// the weights made every size slower (3 to 24 %), as did maxima in front of all weights (7 %).
 #pragma once
 
 #include "afx_paged_attn.cuh"
@@ -63,6 +66,7 @@ struct PrWork {
     int b, kv_head, row_base;  // first of its 256 rows
     int few, low;              // positions: [0, few), then low ..
     int tiles[2];              // tiles of positions that each row tile sees
+    int boxed;                 // tiles of positions that are read in boxes: those in front of the one with the sequence's end
 };
 
 // Pairs of row tiles of a sequence.
@@ -131,6 +135,8 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
             // (rows in front of the sequence see nothing of their one tile)
             w.tiles[x] = r0 >= rows ? 0 : last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 1;
         }
+        const int end = min(s.len, s.first + s.n);
+        w.boxed = args.box == 1 || w.few + end < w.low ? 0 : (w.few + end - w.low) / kPrPos;
         *out = w;
     };
     const bool first_call = longest < 0, report = first_call && blockIdx.x == 0;
@@ -266,13 +272,13 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             const bool lead = elect_one();
             const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
             auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
-            // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies are writes like any thread's, the
-            // products read shared memory by another path: the fence stands between what the barrier says and them.
+            // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies of rows are writes like any thread's,
+            // the products read shared memory by another path: the fence stands between what the barrier says and them.
             int slot = 0;
             uint32_t turn = 0, q_turn = 0, p_turn[2] = {0, 0};
-            auto arrived = [&]() {
+            auto arrived = [&](bool boxed) {
                 const bool in = wait(&bar.full[slot], turn);
-                fence_proxy_async();
+                if (!boxed) fence_proxy_async();
                 return in;
             };
             auto step = [&]() {
@@ -300,7 +306,8 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 if (!ok || w.b < 0) break;
                 const int tiles[2] = {__shfl_sync(0xFFFFFFFFu, w.tiles[0], 0), __shfl_sync(0xFFFFFFFFu, w.tiles[1], 0)};
                 const int nt = max(tiles[0], tiles[1]);
-                ok = wait(&bar.q_full, q_turn) && arrived();
+                const int boxed = __shfl_sync(0xFFFFFFFFu, w.boxed, 0);
+                ok = wait(&bar.q_full, q_turn) && arrived(false);
                 q_turn ^= 1u;
                 if (ok) {
 #pragma unroll
@@ -314,13 +321,15 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     step();
                 }
                 for (int j = 0; ok && j < nt; ++j) {
-                    ok = arrived();
+                    ok = arrived(j < boxed);
                     if (!ok) break;
-                    const int vs = slot;
+                    const int vs = slot, last_x = j < tiles[1] ? 1 : 0;
                     step();
                     const int ks = slot;
+                    // (Waited for here, while products are still being made: in front of the scores the wait is exposed, 930 -> 946 us;
+                    // in front of the last scores of the step before, the copies are not there yet, 1010 us.)
                     if (j + 1 < nt) {
-                        ok = arrived();
+                        ok = arrived(j + 1 < boxed);
                         step();
                         if (!ok) break;
                     }
@@ -341,6 +350,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                         }
                         p_turn[x] ^= 1u;
                         if (!ok) continue;
+                        if (x == last_x && lead) tc_commit(&bar.empty[vs]);
                         if (j + 1 < tiles[x]) {
                             scores(x, ks);
                         } else {
@@ -349,7 +359,6 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                         }
                     }
                     if (ok && lead) {
-                        tc_commit(&bar.empty[vs]);
                         if (j + 1 < nt) tc_commit(&bar.empty[ks]);
                         if (j + 2 == nt) tc_commit(&bar.q_empty);  // the last scores of this work are issued
                     }
@@ -430,9 +439,8 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     }
                     when_landed(&bar.full[slot]);
                 };
-                // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).  The first that is not
-                // holds the sequence's end, or (box = 1) any.
-                const int n_boxed = args.box == 1 || w.few + end < w.low ? 0 : (w.few + end - w.low) / kPrPos;
+                // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).
+                const int n_boxed = w.boxed;
                 int page = -1, in_page = 0;
                 auto look_up_box = [&](int j) {
                     const int v = j * kPrPos + (lane % boxes) * args.box, p = v < w.few ? v : v - w.few + w.low;
