@@ -70,7 +70,8 @@ const char* afx_status_string(afx_status s);
  * Bytes of DEVICE scratch memory the entry points below need for operators of up to K_max
  * channels, N_max outputs and T_max tokens: always 0.  Partial sums meet in shared memory and
  * in the distributed shared memory of a thread-block cluster, and a selection stays inside
- * the consuming kernel or leaves in the caller's list, so no call takes a workspace pointer.  (Interface bookkeeping; the
+ * the consuming kernel or leaves in the caller's list, so none of these calls takes a workspace pointer (afx_moe_block and
+ * the paged cache's attention do, and have functions of their own for its size).  (Interface bookkeeping; the
  * paper has no counterpart.)
  */
 size_t afx_workspace_bytes(int K_max, int N_max, int T_max);

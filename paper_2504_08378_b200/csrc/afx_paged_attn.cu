@@ -43,8 +43,9 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
     if (need != 0 && workspace == nullptr) return AFX_ERR_INVALID_ARG;
     if (workspace_bytes < need) return AFX_ERR_CAPACITY;
     if (a.w.n_seqs == 0 || a.w.n_tokens == 0) return AFX_OK;
-    a.mask.window = window;
-    a.mask.sinks = sinks;
+    // no position reaches 2^30: what is larger says the same, and differences of positions stay inside 32 bits
+    a.mask.window = window < (1 << 30) ? window : 1 << 30;
+    a.mask.sinks = sinks < (1 << 30) ? sinks : 1 << 30;
     a.q = static_cast<const char*>(q);
     a.ldq = ldq;
     a.q_type = q_dtype;

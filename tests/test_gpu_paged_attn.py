@@ -303,3 +303,45 @@ def test_joining_two_caches_by_their_sums():
     tol = attention_tolerance(want, mass, norm, 64, "f16", "f16")[0] + 2.0 ** -11 * (w[..., None] * out.double().abs()).sum(0).numpy()
     assert (np.abs(joined - want[0]) <= tol).all()
     assert np.abs(torch.logsumexp(lse.double(), 0).numpy() - want_lse[0]).max() <= 1e-4
+
+
+@pytest.mark.parametrize("news", [[1, 1], [40, 7], [3, 60]])
+def test_the_largest_windows_and_counts_of_first_positions(news):
+    most = 2 ** 31 - 1
+    for window, sinks in ((most, 0), (most, most), (5, most), (0, most)):
+        p = Problem([200, 61], news, 4, 2, 64, 16, "f16")
+        check(p, window=window if window < most else 10 ** 9, sinks=sinks if sinks < most else 10 ** 9)
+        q = p.randn(p.rows, 4, 64, dtype="f16")
+        kvd = p.upload(afx)
+        assert torch.equal(attend(p, q, kvd, "f16", "f16", window, sinks)[0],
+                           attend(p, q, kvd, "f16", "f16", min(window, 10 ** 9), min(sinks, 10 ** 9))[0])
+
+
+@pytest.mark.parametrize("news", [[2, 1], [40, 9]])
+def test_rows_in_front_of_the_first_sequence_stay(news):
+    p = Problem([100, 61], news, 4, 2, 64, 16, "f16", pad=5)
+    q = p.randn(p.rows, 4, 64, dtype="f16")
+    kvd = p.upload(afx)
+    p.d_start += 3  # three rows in front, two behind
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = attend(p, q, kvd, "f16", "f16", status=status)
+    assert status.item() == 0 and (out[:3] == TORCH_MARK["f16"]).all() and (out[-2:] == TORCH_MARK["f16"]).all()
+    want, _, mass, norm = p.attend(torch.cat((q[3:], q[:3])))
+    n = sum(news)
+    tol = attention_tolerance(want[:n], mass[:n], norm[:n], 64, "f16", "f16")
+    assert (np.abs(out[3:3 + n].double().numpy() - want[:n]) <= tol).all()
+
+
+@pytest.mark.parametrize("every", [1, 7, 40])
+def test_thousands_of_sequences_most_of_them_idle(every):
+    """Every so many sequences has a token (or, seldom, a few dozen): the others take no part."""
+    n = 3000
+    news = [0 if i % every else (30 if i % (every * 50) == 0 else 1 + i % 3) for i in range(n)]
+    lens = [max(m, 1 + (i * 13) % 60) for i, m in enumerate(news)]
+    check(Problem(lens, news, 2, 1, 64, 16, "f16"))
+
+
+@pytest.mark.parametrize("cache,dim,heads,kv", [("bf16", 128, 16, 2), ("f16", 64, 6, 3)])
+def test_prompts_beside_decoding_sequences(cache, dim, heads, kv):
+    check(Problem([700, 333, 900, 60, 1, 2000, 12], [300, 1, 9, 60, 1, 8, 12], heads, kv, dim, 16, cache, pad=1))
+    check(Problem([700, 333, 900, 60, 1, 2000, 12], [300, 1, 9, 60, 1, 8, 12], heads, kv, dim, 48, cache, pad=1), window=100, sinks=5)
