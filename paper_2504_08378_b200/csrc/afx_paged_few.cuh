@@ -112,11 +112,14 @@ struct FewScratch {
     FewStart start;
 };
 // The list's length.  All threads of the block call it.
-__device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* sc, bool report, int64_t& mine_before, int64_t& mine) {
+// (last: the last of this thread's sequences)
+__device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* sc, bool report, int64_t& mine_before, int64_t& mine,
+                                            FewSeq& last) {
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads, tid = threadIdx.x;
     mine = 0;
     for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
         const FewSeq q = few_seq(f, i, report);
+        last = q;
         mine += static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
     }
     int64_t incl = mine;
@@ -137,9 +140,14 @@ __device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* s
     return total;
 }
 // The thread among whose sequences unit `at` lies writes down which.
-__device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int64_t mine_before, int64_t mine) {
+__device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int64_t mine_before, int64_t mine,
+                                         const FewSeq& last) {
     if (at < mine_before || at >= mine_before + mine) return;
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads;
+    if (per == 1) {
+        sc->start = {mine_before, last, static_cast<int>(threadIdx.x)};
+        return;
+    }
     for (int b = threadIdx.x * per; b < min(n, static_cast<int>(threadIdx.x + 1) * per); ++b) {
         const FewSeq q = few_seq(f, b, false);
         const int64_t t = static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
@@ -271,6 +279,13 @@ __device__ __forceinline__ bool few_sees(const PagedMask& m, int pos, int p) {
     return p <= pos && (m.window == 0 || p > pos - m.window || p < m.sinks);
 }
 
+// Where value d of row r lies among the sums that meet: blocks of 8 values change places by the row (all rows of a product
+// at the same banks otherwise).
+template <int DW>
+__device__ __forceinline__ int few_place(int r, int d) {
+    return r * DW + (d ^ ((r & 7) << 3));
+}
+
 // Four dims of a finished row; nothing seen: zeros.
 template <int D>
 __device__ __forceinline__ void few_store(const PagedFewArgs& f, int t, int h, int d, const float4& s, float M, float L) {
@@ -332,13 +347,14 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         con.more = true;
     } else {
         int64_t mine_before, mine;
-        const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine);
+        FewSeq last;
+        const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine, last);
         ranges = FewRanges(total, gridDim.x);
         if (tid == 0) f.joins[my].last = -1;  // (a later piece may say otherwise)
         if (my >= ranges.n) return;
         const int64_t lo = ranges.begin(my);
         hi = ranges.begin(my + 1);
-        few_find(f, &scratch, lo, mine_before, mine);
+        few_find(f, &scratch, lo, mine_before, mine, last);
         __syncthreads();
         con.b = scratch.start.b;
         con.q = scratch.start.q;
@@ -399,6 +415,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    if (con.more) warm_queries(con);
     int64_t ahead;  // the chunk behind those on their way: looked up a chunk's time before it is wanted
     {
         int64_t off[ST - 1];
@@ -627,7 +644,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
 #pragma unroll
                 for (int e = 0; e < NR; ++e) {
                     const float* t = &o[part * (DW / 8) + i][2 * e];
-                    *reinterpret_cast<float2*>(mine + (gid + 8 * e) * DW + 8 * i + 2 * tig) = make_float2(t[0], t[1]);
+                    *reinterpret_cast<float2*>(mine + few_place<DW>(gid + 8 * e, 8 * i + 2 * tig)) = make_float2(t[0], t[1]);
                 }
             __syncwarp();
             for (uint32_t left = bad; left != 0; left &= left - 1) {  // again, over what the row sees alone
@@ -650,7 +667,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
 #pragma unroll
                 for (int x = 0; x < D / 32; ++x) {
                     const int d = lane * (D / 32) + x - part * DW;
-                    if (d >= 0 && d < DW) mine[r * DW + d] = st.acc[x];
+                    if (d >= 0 && d < DW) mine[few_place<DW>(r, d)] = st.acc[x];
                 }
                 if (lane == 0) {
                     sm_m[warp][r] = st.m;
@@ -672,7 +689,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                 float4 s4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float4 t = *reinterpret_cast<const float4*>(merge(w) + x);
+                    const float4 t = *reinterpret_cast<const float4*>(merge(w) + few_place<DW>(r, x % DW));
                     const float wt = sm_m[w][r] == -INFINITY ? 0.0f : fast_exp2(sm_m[w][r] - M);
                     if (wt == 0.0f && sm_l[w][r] == 0.0f) continue;
                     L = fmaf(wt, sm_l[w][r], L);
