@@ -112,8 +112,9 @@ __device__ __forceinline__ void store_piece(char* row, int type, int piece, cons
 // is not rotated in pairs of pieces behind), so that the rotation needs no exchange and its cosines are loaded once
 // per token.  A row's norm is a sum over its lanes (shuffles).  Everything is held in fp32 and rounded once when it is stored.
 template <int D, int XT>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(AppendArgs a) {
     constexpr int GL = D / 16, RPP = kAppendThreads / GL, XB = XT == AFX_F32 ? 4 : 2;
+    __shared__ float4 rot[2][D / 8];  // of the token's position
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = blockIdx.x, l = threadIdx.x % GL;
@@ -169,17 +170,12 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
     const int page = paged_page(a.w, b, pos, in_page);
     if (page < 0 && lead) report_status(a.w.status, AFX_ERR_INVALID_ARG);
     const int64_t cell = page * a.w.page_stride + in_page * a.w.pos_stride;
-    float cs[8], sn[8];
-    if (rotates) {
-        const float4* c4 = reinterpret_cast<const float4*>(a.cos + static_cast<int64_t>(pos) * a.half) + 2 * l;
-        const float4* s4 = reinterpret_cast<const float4*>(a.sin + static_cast<int64_t>(pos) * a.half) + 2 * l;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float4 c = c4[j], n = s4[j];
-            cs[4 * j] = c.x; cs[4 * j + 1] = c.y; cs[4 * j + 2] = c.z; cs[4 * j + 3] = c.w;
-            sn[4 * j] = n.x; sn[4 * j + 1] = n.y; sn[4 * j + 2] = n.z; sn[4 * j + 3] = n.w;
-        }
+    // (in shared memory: 16 registers more would leave room for three blocks per SM instead of four)
+    if (threadIdx.x < static_cast<unsigned>(a.half) / 2) {
+        const int part = threadIdx.x & 1, at = threadIdx.x >> 1;  // cosines and sines, four at a time
+        rot[part][at] = reinterpret_cast<const float4*>((part == 0 ? a.cos : a.sin) + static_cast<int64_t>(pos) * a.half)[at];
     }
+    __syncthreads();
     for (; r - static_cast<int>(threadIdx.x) / GL < r_end; r += RPP) {  // (all lanes of a warp leave together)
         const bool live = r < r_end;
         const Piece<XT> ca = na, cb = nb;
@@ -227,6 +223,13 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(AppendArgs a) {
             continue;
         }
         if (rotates) {
+            float cs[8], sn[8];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float4 c = rot[0][2 * l + j], n = rot[1][2 * l + j];
+                cs[4 * j] = c.x; cs[4 * j + 1] = c.y; cs[4 * j + 2] = c.z; cs[4 * j + 3] = c.w;
+                sn[4 * j] = n.x; sn[4 * j + 1] = n.y; sn[4 * j + 2] = n.z; sn[4 * j + 3] = n.w;
+            }
             if (a.style == AFX_ROPE_HALVES) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
