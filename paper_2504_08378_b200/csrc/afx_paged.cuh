@@ -55,11 +55,16 @@ __device__ __forceinline__ SeqSpan paged_span(const PagedView& w, int b, bool re
     return s;
 }
 
-// Page of position p (0 <= p < cap) of sequence b and the place in it; -1 where the table's entry is no page.
-__device__ __forceinline__ int paged_page(const PagedView& w, int b, int p, int& in_page) {
+// The table's entry for position p (0 <= p < cap) of sequence b as it stands there, and the place in the page.
+__device__ __forceinline__ int paged_entry(const PagedView& w, int b, int p, int& in_page) {
     const int i = static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(p)) * w.mul) >> (31 + w.shift));
     in_page = p - i * w.page_size;
-    const int page = w.table[static_cast<int64_t>(b) * w.table_stride + i];
+    return w.table[static_cast<int64_t>(b) * w.table_stride + i];
+}
+
+// The page of that position; -1 where the entry is none.
+__device__ __forceinline__ int paged_page(const PagedView& w, int b, int p, int& in_page) {
+    const int page = paged_entry(w, b, p, in_page);
     return static_cast<uint32_t>(page) < static_cast<uint32_t>(w.n_pages) ? page : -1;
 }
 

@@ -380,26 +380,39 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
             }
         }
     };
-    // lane j < 16: offset of position j of the next chunk (-1: leave out); moves on
-    auto look_up = [&]() -> int64_t {
+    // Lane j < 16: where position j of the next chunk lies.  The table's entry is not looked at here, but when the chunk is
+    // requested: nobody waits for it meanwhile.  Moves on.
+    struct Ahead {
+        int64_t rest;  // what comes to the page's offset
+        int page;
+        int kind;      // 0: a position, -1: behind the last one, -2: there is no chunk (the same for all lanes)
+    };
+    auto look_up = [&]() -> Ahead {
         while (pro.more && pk >= pn) {
             pro.next(f);
             pk = 0;
             pn = pro.more ? pro.chunks<W>(warp) : 0;
             if (pro.more) warm_queries(pro);
         }
-        if (!pro.more) return -2;
+        Ahead a = {0, 0, -2};
+        if (!pro.more) return a;
         const int v = ((pro.t0 + pk) * W + warp) * kFewChunk + (lane & 15);
         ++pk;
-        if (v >= pro.q.nv) return -1;
-        const int64_t at = paged_row(f.a.w, pro.b, few_pos(pro.q, v), pro.kv_head);
-        if (at < 0) report_status(f.a.w.status, AFX_ERR_INVALID_ARG);
-        return at;
+        a.kind = v < pro.q.nv ? 0 : -1;
+        if (a.kind == 0) {
+            int in_page;
+            a.page = paged_entry(f.a.w, pro.b, few_pos(pro.q, v), in_page);
+            a.rest = in_page * f.a.w.pos_stride + pro.kv_head * f.a.w.head_stride;
+        }
+        return a;
     };
-    auto issue = [&](int64_t p_off) {  // (-2: no chunk; the same for all lanes)
-        if (p_off != -2) {
+    auto issue = [&](const Ahead& a) {
+        if (a.kind != -2) {
+            const bool good = a.kind == 0 && static_cast<uint32_t>(a.page) < static_cast<uint32_t>(f.a.w.n_pages);
+            if (a.kind == 0 && !good) report_status(f.a.w.status, AFX_ERR_INVALID_ARG);
+            const int64_t p_off = good ? a.page * f.a.w.page_stride + a.rest : -1;
             const uint32_t at = ring + p_stage * Cfg::kChunkBytes;
-            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, p_off >= 0) & 0xFFFFu;
+            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, good) & 0xFFFFu;
             if (lane == 0) stage_mask[warp][p_stage] = mask;
             constexpr int RPI = 32 / PIECES;  // rows per instruction
 #pragma unroll
@@ -416,9 +429,9 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     if (con.more) warm_queries(con);
-    int64_t ahead;  // the chunk behind those on their way: looked up a chunk's time before it is wanted
+    Ahead ahead;  // the chunk behind those on their way: looked up a chunk's time before it is wanted
     {
-        int64_t off[ST - 1];
+        Ahead off[ST - 1];
 #pragma unroll
         for (int i = 0; i < ST - 1; ++i) off[i] = look_up();
         ahead = look_up();
