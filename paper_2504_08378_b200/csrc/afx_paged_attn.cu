@@ -19,7 +19,7 @@ static afx_status attn_args(const afx_paged_kv* kv, int n_heads, int32_t* dev_st
 extern "C" size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads) {
     afx::PagedAttnArgs a = {};
     if (afx::attn_args(kv, n_heads, nullptr, &a) != AFX_OK) return 0;
-    if (kv->max_new > AFX_MAX_T && kv->n_seqs <= 1) return 0;
+    if (kv->n_seqs <= 1 && kv->max_new > afx::few_most_tokens(a.rep, afx::kFewMostGroups)) return 0;
     return (afx::few_workspace_bytes(kv->head_dim) + 255) / 256 * 256;
 }
 
@@ -54,18 +54,20 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
     a.out_type = out_dtype;
     a.lse = lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // Sequences with up to AFX_MAX_T new tokens are split over their positions; the tiles of 128 rows are for those
-    // with more.  A batch may have both (a few prompts' chunks beside sequences that decode): one kernel after the other, each
-    // leaving out what is the other's.
-    const bool prompts = kv->max_new > AFX_MAX_T;
+    // Sequences with few new tokens are split over their positions; the tiles of 128 rows are for those with more.  A batch may
+    // have both (a few prompts' chunks beside sequences that decode): one kernel after the other, each leaving out what is the other's.
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    const int64_t groups = sms / (static_cast<int64_t>(a.w.n_seqs) * a.w.n_kv);
+    const int most = few_most_tokens(a.rep, static_cast<int>(groups < kFewMostGroups ? groups : kFewMostGroups));
+    const bool prompts = kv->max_new > most;
     if (!prompts || kv->n_seqs > 1) {
         PagedFewArgs f = {};
         f.a = a;
-        f.most = AFX_MAX_T;
+        f.most = most;
         f.joins = static_cast<FewJoin*>(workspace);
         f.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_slots_at());
         const afx_status few = launch_paged_few(kv->dtype, D, f, st);
         if (few != AFX_OK || !prompts) return few;
     }
-    return launch_paged_prompt(kv->dtype, D, a, kv->n_seqs > 1 ? AFX_MAX_T : 0, st);
+    return launch_paged_prompt(kv->dtype, D, a, kv->n_seqs > 1 ? most : 0, st);
 }

@@ -69,6 +69,16 @@ struct PagedFewArgs {
     float* slots;
 };
 
+// Most new tokens of a sequence that these kernels take: AFX_MAX_T, or what makes `groups` groups of 16 rows.  More groups than
+// AFX_MAX_T tokens have cost more products than a tile of 128 rows, but use the whole machine where the tiles are few: with up
+// to as many groups as SMs in a call this is the faster way (a sequence of 4000 positions, 32 / 8 heads: 16 new tokens 16 us, by
+// tiles 60, 32 new tokens 25 and 61; 32000 positions and 32 new tokens 144 and 417; 32 / 32 heads, 48 new tokens 43 and 61); beyond,
+// the slower (32 / 32 heads, 128 new tokens at 1000 positions 30 and 23; 64 sequences of 16 new tokens at 2000 positions 329 and 154).
+constexpr int kFewMostGroups = 16;
+inline int few_most_tokens(int rep, int groups) {
+    const int by_groups = groups * 16 / rep;
+    return by_groups > AFX_MAX_T ? by_groups : AFX_MAX_T;
+}
 afx_status launch_paged_few(int dtype, int D, PagedFewArgs& f, cudaStream_t st);  // afx_paged_few.cu
 inline bool few_packed(int max_new, int rep) { return static_cast<int64_t>(max_new) * rep <= 8; }
 

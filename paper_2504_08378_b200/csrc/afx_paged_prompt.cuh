@@ -43,6 +43,7 @@ struct PagedPromptArgs {
     PagedAttnArgs a;
     int box;   // positions of a tensor copy; 1: none are made
     int skip;  // sequences of up to that many new tokens are somebody else's
+    int rows;  // of a work: both row tiles' 256, or 128 (the second tile has none)
 };
 
 afx_status launch_paged_prompt(int dtype, int D, const PagedAttnArgs& a, int skip, cudaStream_t st);  // afx_paged_prompt.cu
@@ -69,27 +70,25 @@ struct PrWork {
     int boxed;                 // tiles of positions that are read in boxes: those in front of the one with the sequence's end
 };
 
-// Pairs of row tiles of a sequence.
-__device__ __forceinline__ int pr_pairs(const PagedPromptArgs& g, const SeqSpan& s) {
-    constexpr int R = kPrTiles * kPrRows;
-    return s.n > g.skip ? static_cast<int>((static_cast<int64_t>(s.n) * g.a.rep + R - 1) / R) : 0;
+// Works of a sequence and kv head.
+__device__ __forceinline__ int pr_works(const PagedPromptArgs& g, const SeqSpan& s) {
+    return s.n > g.skip ? static_cast<int>((static_cast<int64_t>(s.n) * g.a.rep + g.rows - 1) / g.rows) : 0;
 }
-// A pair's work goes by the positions that its last row sees; pair i of a sequence: min(window and first positions, first + 1 +
-// (256 (i + 1) - 1) / rep).  The largest of a sequence, and how many of its n pairs have at least `least`.
+// A work is as long as what its last row sees; work i of a sequence: min(window and first positions, first + 1 +
+// (rows (i + 1) - 1) / rep).  The largest of a sequence, and how many of its n works have at least `least`.
 __device__ __forceinline__ int pr_seen_at_most(const PagedAttnArgs& a) {
     return a.mask.window > 0 ? min(a.mask.window, 1 << 29) + min(a.mask.sinks, 1 << 29) : 0x7FFFFFFF;
 }
-__device__ __forceinline__ int pr_most(const PagedAttnArgs& a, const SeqSpan& s, int n) {
-    return n > 0 ? min(pr_seen_at_most(a), max(s.first + 1 + static_cast<int>((static_cast<int64_t>(n) * kPrTiles * kPrRows - 1) / a.rep), 1)) : 0;
+__device__ __forceinline__ int pr_most(const PagedPromptArgs& g, const SeqSpan& s, int n) {
+    return n > 0 ? min(pr_seen_at_most(g.a), max(s.first + 1 + static_cast<int>((static_cast<int64_t>(n) * g.rows - 1) / g.a.rep), 1)) : 0;
 }
-__device__ __forceinline__ int pr_count(const PagedAttnArgs& a, const SeqSpan& s, int n, int least) {
-    if (pr_seen_at_most(a) < least) return 0;
-    constexpr int R = kPrTiles * kPrRows;
-    const int64_t need = static_cast<int64_t>(least) - 1 - s.first;  // (256 (i + 1) - 1) / rep >= need
-    const int64_t from = need <= 0 ? 0 : max((need * a.rep + 1 + R - 1) / R - 1, int64_t{0});
+__device__ __forceinline__ int pr_count(const PagedPromptArgs& g, const SeqSpan& s, int n, int least) {
+    if (pr_seen_at_most(g.a) < least) return 0;
+    const int64_t need = static_cast<int64_t>(least) - 1 - s.first;  // (rows (i + 1) - 1) / rep >= need
+    const int64_t from = need <= 0 ? 0 : max((need * g.a.rep + g.rows) / g.rows - 1, int64_t{0});
     return static_cast<int>(max(n - from, int64_t{0}));
 }
-constexpr int kPrClasses = 4;  // pairs with more than 1/2, 1/4, 1/8 of the longest one's positions, and the others
+constexpr int kPrClasses = 4;  // works with more than 1/2, 1/4, 1/8 of the longest one's positions, and the others
 
 // Bits 0 .. n - 1 of a word (n <= 0: none, n >= 32: all).
 __device__ __forceinline__ uint32_t pr_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u; }
@@ -112,19 +111,19 @@ __device__ __forceinline__ uint32_t pr_weights(float s0, float s1, f32x2 scale, 
     return pack2_bits<CT>(p0, p1);
 }
 
-// Work `place` of the grid: (pair of row tiles, kv head), kv heads side by side; the pairs in classes of falling length (a long one
+// Work `place` of the grid: (rows, kv head), kv heads side by side; the works in classes of falling length (a long one
 // that begins last is what everybody waits for), in a class sequence by sequence.  One warp; what it finds goes to
 // *out, nothing when there are not so many.  longest: -1 on the warp's first call.
 __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, int& longest, PrWork* out) {
     const PagedAttnArgs& a = args.a;
     const int pair = place / a.w.n_kv, lane = lane_id();
-    auto take = [&](const SeqSpan& s, int b, int i) {  // pair i of sequence b
+    auto take = [&](const SeqSpan& s, int b, int i) {  // work i of sequence b
         PrWork w;
         w.s = s;
         w.b = b;
         w.kv_head = place - pair * a.w.n_kv;
-        w.row_base = i * kPrTiles * kPrRows;
-        const int rows = s.n * a.rep;
+        w.row_base = i * args.rows;
+        const int rows = min(s.n * a.rep, w.row_base + args.rows);
         const int first = max(s.first + w.row_base / a.rep, 0);
         // (both on a box's border; places that no row sees are masked)
         w.low = paged_low(a.mask, first) & ~(args.box - 1);
@@ -144,7 +143,7 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         longest = 0;
         if (lane == 0) {
             const SeqSpan s = paged_span(a.w, 0, report);
-            const int t = pr_pairs(args, s);
+            const int t = pr_works(args, s);
             if (pair < t) take(s, 0, t - 1 - pair);
         }
         return;
@@ -154,21 +153,21 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         longest = 0;
         for (int i = i0; i < i1; ++i) {
             const SeqSpan s = paged_span(a.w, i, report);
-            longest = max(longest, pr_most(a, s, pr_pairs(args, s)));
+            longest = max(longest, pr_most(args, s, pr_works(args, s)));
         }
         longest = __reduce_max_sync(0xFFFFFFFFu, longest);
     }
-    int before = 0;  // pairs of the classes in front
+    int before = 0;  // works of the classes in front
     for (int c = 0; c < kPrClasses; ++c) {
         const int most = (longest >> c) + 1, least = (longest >> (c + 1)) + 1;
         auto in_class = [&](const SeqSpan& s, int t, int& up) {
-            up = c > 0 ? pr_count(a, s, t, most) : 0;
-            return (c + 1 < kPrClasses ? pr_count(a, s, t, least) : t) - up;
+            up = c > 0 ? pr_count(args, s, t, most) : 0;
+            return (c + 1 < kPrClasses ? pr_count(args, s, t, least) : t) - up;
         };
         int mine = 0, up;
         for (int i = i0; i < i1; ++i) {
             const SeqSpan s = paged_span(a.w, i, false);
-            mine += in_class(s, pr_pairs(args, s), up);
+            mine += in_class(s, pr_works(args, s), up);
         }
         int incl = mine;
 #pragma unroll
@@ -181,7 +180,7 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         if (pair >= at && pair < at + mine) {
             for (int i = i0; i < i1; ++i) {
                 const SeqSpan s = paged_span(a.w, i, false);
-                const int t = pr_pairs(args, s), k = in_class(s, t, up);
+                const int t = pr_works(args, s), k = in_class(s, t, up);
                 if (pair - at < k) {
                     take(s, i, t - 1 - (up + pair - at));
                     break;
@@ -401,7 +400,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 PrWork w;
                 ok = next_work(it, w);
                 if (!ok || w.b < 0) break;
-                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.s.n * a.rep;
+                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = min(w.s.n * a.rep, w.row_base + args.rows);
                 if (lw == 2) {  // a place in the grid whose block has not begun, if there is one
                     asked = it + 1;
                     if (lane == 0) {
@@ -558,7 +557,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             PrWork w;
             ok = next_work(it, w);
             if (!ok || w.b < 0) break;
-            const int rows = w.s.n * a.rep;
+            const int rows = min(w.s.n * a.rep, w.row_base + args.rows);
             const int rr = w.row_base + x * kPrRows + (warp & 3) * 32 + lane;
             const int i = rr / a.rep, h = w.kv_head * a.rep + rr - i * a.rep;
             const bool live = rr < rows;
