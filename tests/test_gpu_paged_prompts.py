@@ -162,3 +162,25 @@ def test_more_works_than_multiprocessors(dim, page, window):
     """Several hundred works of unlike length: blocks take over others' places."""
     lens = [700, 300, 420, 301, 1000, 333]
     check(Problem(lens, [300, 300, 20, 290, 40, 333], 20, 20, dim, page, "bf16"), window=window, sinks=3)
+
+
+@pytest.mark.parametrize("page", [16, 64, 10])
+@pytest.mark.parametrize("lens,news", [([400], [1]), ([400, 333], [8, 3]), ([700], [300]), busy([700], [120])])
+def test_pages_in_front_of_a_window_may_be_gone(page, lens, news):
+    """What lies in front of every new token's window (and behind the first positions) is not touched, its pages' entries included."""
+    window, sinks = 50, 5
+    p = Problem(lens, news, 4, 2, 64, page, "f16")
+    q = p.randn(p.rows, 4, 64, dtype="f16")
+    kvd = p.upload(afx)
+    gone = 0
+    for b, (n, new) in enumerate(zip(p.lens, p.news)):
+        low = max(0, n - new - window + 1) if new else 0
+        for i in range(-(-sinks // page), low // page):
+            p.d_table[b, i] = -1
+            gone += 1
+    assert gone > 0
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, _ = attend(p, q, kvd, "f16", "f16", window, sinks, status=status)
+    assert status.item() == 0
+    want, _, mass, norm = p.attend(q, window, sinks)
+    assert (np.abs(out.double().numpy() - want) <= attention_tolerance(want, mass, norm, 64, "f16", "f16")).all()
