@@ -63,8 +63,9 @@ struct PrBarriers {
 
 // A work: what a block does at a time.
 struct PrWork {
-    SeqSpan s;
-    int b, kv_head, row_base;  // first of its 256 rows
+    int row0, first, end;      // the sequence's first token row and its position; the position behind its last one
+    int b, kv_head;
+    int row_base, rows;        // its rows of (token, query head of the kv head): row_base .. rows - 1
     int few, low;              // positions: [0, few), then low ..
     int tiles[2];              // tiles of positions that each row tile sees
     int boxed;                 // tiles of positions that are read in boxes: those in front of the one with the sequence's end
@@ -119,11 +120,13 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
     const int pair = place / a.w.n_kv, lane = lane_id();
     auto take = [&](const SeqSpan& s, int b, int i) {  // work i of sequence b
         PrWork w;
-        w.s = s;
+        w.row0 = s.row0;
+        w.first = s.first;
+        w.end = min(s.len, s.first + s.n);
         w.b = b;
         w.kv_head = place - pair * a.w.n_kv;
         w.row_base = i * args.rows;
-        const int rows = min(s.n * a.rep, w.row_base + args.rows);
+        const int rows = w.rows = min(s.n * a.rep, w.row_base + args.rows);
         const int first = max(s.first + w.row_base / a.rep, 0);
         // (both on a box's border; places that no row sees are masked)
         w.low = paged_low(a.mask, first) & ~(args.box - 1);
@@ -134,8 +137,7 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
             // (rows in front of the sequence see nothing of their one tile)
             w.tiles[x] = r0 >= rows ? 0 : last >= w.low ? (w.few + last + 1 - w.low + kPrPos - 1) / kPrPos : 1;
         }
-        const int end = min(s.len, s.first + s.n);
-        w.boxed = args.box == 1 || w.few + end < w.low ? 0 : (w.few + end - w.low) / kPrPos;
+        w.boxed = args.box == 1 || w.few + w.end < w.low ? 0 : (w.few + w.end - w.low) / kPrPos;
         *out = w;
     };
     const bool first_call = longest < 0, report = first_call && blockIdx.x == 0;
@@ -400,7 +402,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 PrWork w;
                 ok = next_work(it, w);
                 if (!ok || w.b < 0) break;
-                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = min(w.s.n * a.rep, w.row_base + args.rows);
+                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.rows;
                 if (lw == 2) {  // a place in the grid whose block has not begun, if there is one
                     asked = it + 1;
                     if (lane == 0) {
@@ -409,7 +411,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     }
                     __syncwarp();
                 }
-                const int end = min(w.s.len, w.s.first + w.s.n);
+                const int end = w.end;
                 int64_t off[3], next[3];
                 auto look_up = [&](int j) {
 #pragma unroll
@@ -495,7 +497,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                         q_used = true;
                         for (int blk = lw; blk < kPrTiles * kPrRows / 32; blk += kPrLoaders) {
                             const int rr = w.row_base + blk * 32 + lane, i = rr / a.rep;
-                            const int64_t from = rr < rows ? (w.s.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D : -1;
+                            const int64_t from = rr < rows ? (w.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D : -1;
 #pragma unroll
                             for (int k = 0; k < 32 / RPI; ++k) {
                                 const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
@@ -557,19 +559,19 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             PrWork w;
             ok = next_work(it, w);
             if (!ok || w.b < 0) break;
-            const int rows = min(w.s.n * a.rep, w.row_base + args.rows);
+            const int rows = w.rows;
             const int rr = w.row_base + x * kPrRows + (warp & 3) * 32 + lane;
             const int i = rr / a.rep, h = w.kv_head * a.rep + rr - i * a.rep;
             const bool live = rr < rows;
-            const int pos = live ? w.s.first + i : -1;
+            const int pos = live ? w.first + i : -1;
             const int shift = w.few - w.low;  // place in the list of visible positions = position + shift, behind the first ones
             const int v_hi = pos + shift;     // the row sees places <= v_hi that are >= v_lo or < v_few
             const int v_lo = a.mask.window > 0 ? pos - a.mask.window + 1 + shift : 0;
             const int v_few = a.mask.window > 0 ? a.mask.sinks : 0;  // (first positions are their own places: few covers them, or few = low)
             // places that every row of the tile sees: below v_few and [lo_all, hi_all]
             const int rr0 = w.row_base + x * kPrRows, rr1 = min(rr0 + kPrRows, rows) - 1;
-            const int hi_all = w.s.first + rr0 / a.rep + shift;
-            const int lo_all = a.mask.window > 0 ? w.s.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
+            const int hi_all = w.first + rr0 / a.rep + shift;
+            const int lo_all = a.mask.window > 0 ? w.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; ok && j < w.tiles[x]; ++j) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.s_full[x], s_turn, &gave_up));
@@ -672,7 +674,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             }
             // ---- the rows leave.  (Straight from the threads: staged in shared memory they would leave in whole lines, but the
             // next work's queries are on their way into the room for that.)
-            const int64_t at = static_cast<int64_t>(w.s.row0 + i) * a.heads + h;
+            const int64_t at = static_cast<int64_t>(w.row0 + i) * a.heads + h;
             float o[D];
             if (w.tiles[x] > 0) {
 #pragma unroll
@@ -726,14 +728,14 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     st.acc[e] = 0.0f;
-                    q[e] = a.scale * typed_value(a.q, a.q_type, (w.s.row0 + wi) * a.ldq + static_cast<int64_t>(wh) * D + lane * E + e);
+                    q[e] = a.scale * typed_value(a.q, a.q_type, (w.row0 + wi) * a.ldq + static_cast<int64_t>(wh) * D + lane * E + e);
                 }
                 if (wp >= 0) {
                     const int low = paged_low(a.mask, wp);
                     attend_row<D, CT>(a.w, w.b, w.kv_head, q, 0, paged_few(a.mask, low), st);
                     attend_row<D, CT>(a.w, w.b, w.kv_head, q, low, wp + 1, st);
                 }
-                const int64_t wat = static_cast<int64_t>(w.s.row0 + wi) * a.heads + wh;
+                const int64_t wat = static_cast<int64_t>(w.row0 + wi) * a.heads + wh;
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     a.out[wat * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
