@@ -224,3 +224,26 @@ def test_offsets_beyond_32_bits():
     assert ((out.double() - want).abs() <= 2.0 ** -11 * want.abs() + 2.0 ** -25 + 2.0 ** -10 * mass).all()
     del k, v
     torch.cuda.empty_cache()
+
+
+def test_buffers_that_begin_on_any_16_bytes():
+    p = Problem([20, 7], [3, 1], 4, 2, 64, 8, "f16")
+    x = p.randn(p.rows, 8 * 64, dtype="f16")
+    kvd = p.upload(afx)
+    cos, sin = (t.cuda() for t in rope_table(20, 64))
+    outs = []
+    for shift in (0, 16):
+        p.d_both.copy_(p.both)
+        room = [torch.zeros(n * 4 + 16, dtype=torch.uint8, device="cuda") for n in (x.numel(), 20 * 32, 20 * 32, p.rows * 256)]
+        dx = room[0][shift:shift + x.numel() * 2].view(torch.float16).view(x.shape)
+        dx.copy_(x)
+        tabs = [r[shift:shift + 20 * 32 * 4].view(torch.float32).view(20, 32) for r in room[1:3]]
+        tabs[0].copy_(cos)
+        tabs[1].copy_(sin)
+        q_out = room[3][shift:shift + p.rows * 512].view(torch.float16)
+        prep = afx.HeadPrep(x_dtype=0, n_heads=4, eps=1e-5, rope_style=2, rotary_dim=64, rope_len=20, rope_cos=tabs[0].data_ptr(),
+                            rope_sin=tabs[1].data_ptr())
+        afx.afx_paged_append(kvd, prep, dx, 512, dx.data_ptr() + 512, 512, dx.data_ptr() + 768, 512, q_out, "f16")
+        torch.cuda.synchronize()
+        outs.append((p.d_both.clone().view(torch.int16), q_out.clone()))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and outs[0][1].any()

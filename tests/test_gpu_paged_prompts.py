@@ -184,3 +184,65 @@ def test_pages_in_front_of_a_window_may_be_gone(page, lens, news):
     assert status.item() == 0
     want, _, mass, norm = p.attend(q, window, sinks)
     assert (np.abs(out.double().numpy() - want) <= attention_tolerance(want, mass, norm, 64, "f16", "f16")).all()
+
+
+def shifted(t):
+    """The same values 16 bytes behind an allocation's start (which is a multiple of 256)."""
+    room = torch.empty(t.untyped_storage().nbytes() + 16, dtype=torch.uint8, device="cuda")
+    assert room.data_ptr() % 256 == 0
+    flat = room[16:].view(t.dtype)
+    out = torch.as_strided(flat, t.shape, t.stride())
+    out.copy_(t)
+    return out
+
+
+@pytest.mark.parametrize("news", [[1, 1], [5, 8], [300, 20]])
+@pytest.mark.parametrize("cache,dim", [("bf16", 128), ("f16", 64)])
+def test_buffers_that_begin_on_any_16_bytes(news, cache, dim):
+    p = Problem([320, 90], news, 4, 2, dim, 16, cache, pad=1)
+    q = p.randn(p.rows, 4, dim, dtype=cache)
+    kvd = p.upload(afx)
+    pool = shifted(p.d_both)
+    kvd.k_pages, kvd.v_pages = pool[:, 0].data_ptr(), pool[:, 1].data_ptr()
+    dq, out = shifted(q.cuda()), shifted(torch.full((p.rows, 4, dim), 5.0, dtype=TORCH[cache], device="cuda"))
+    n = afx.afx_paged_attn_workspace_bytes(kvd, 4)
+    ws = torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+    afx.afx_paged_attn(kvd, dq, cache, 4 * dim, 4, 0.0, 0, 0, out, cache, None, ws, n)
+    torch.cuda.synchronize()
+    want, _, mass, norm = p.attend(q)
+    live = sum(news)
+    tol = attention_tolerance(want[:live], mass[:live], norm[:live], dim, cache, cache)
+    assert (np.abs(out.cpu().double().numpy()[:live] - want[:live]) <= tol).all() and (out[live:] == 5.0).all()
+
+
+@pytest.mark.parametrize("page,new", [(256, 300), (250, 300), (256, 40)])
+def test_prompts_in_a_pool_beyond_32_bits(page, new):
+    """A pool of more than 2^32 values: tensor copies, rows and the few tokens' split all reach its last pages."""
+    kv, dim, n = 8, 128, 500
+    n_pages = (1 << 32) // (kv * dim * page) + 8
+    k = torch.zeros((n_pages, page, kv, dim), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    table = torch.tensor([[n_pages - 1, n_pages - 3]], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for c in (k, v):
+        c[n_pages - 1] = torch.randn((page, kv, dim), generator=g, device="cuda").bfloat16()
+        c[n_pages - 3] = torch.randn((page, kv, dim), generator=g, device="cuda").bfloat16()
+    length = torch.tensor([n], dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    kvd = afx.PagedKV(dtype=1, n_kv_heads=kv, head_dim=dim, page_size=page, n_pages=n_pages, n_seqs=1, n_tokens=new, max_new=new,
+                      page_stride=page * kv * dim, pos_stride=kv * dim, head_stride=dim, table_stride=2, k_pages=k.data_ptr(),
+                      v_pages=v.data_ptr(), page_table=table.data_ptr(), seq_len=length.data_ptr(), tok_start=start.data_ptr())
+    q = torch.randn((new, kv, dim), generator=g, device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    nb = afx.afx_paged_attn_workspace_bytes(kvd, kv)
+    ws = torch.empty(max(nb, 1), dtype=torch.uint8, device="cuda")
+    afx.afx_paged_attn(kvd, q, "bf16", kv * dim, kv, 0.0, 0, 0, out, "bf16", None, ws, nb)
+    K, V = (torch.cat((t[n_pages - 1], t[n_pages - 3]))[:n].double() for t in (k, v))
+    s = torch.einsum("thd,phd->thp", q.double(), K) / dim ** 0.5
+    pos = n - new + torch.arange(new, device="cuda")
+    s = s.masked_fill(torch.arange(n, device="cuda")[None, None] > pos[:, None, None], -1e300)
+    w = torch.softmax(s, -1)
+    want, mass = torch.einsum("thp,phd->thd", w, V), torch.einsum("thp,phd->thd", w, V.abs())
+    assert ((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1.1 * 2.0 ** -8 * mass).all()
+    del k, v, c
+    torch.cuda.empty_cache()
