@@ -763,7 +763,8 @@ size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_heads);
  * of the token's sequence and kv head h / (n_heads / n_kv_heads).  With the token at position p, j is visible when
  * j <= p and (window = 0, or j > p - window, or j < sinks): a sliding window and a few first positions that stay visible.
  * A token that sees nothing, or only scores of -inf, gets zeros (lse: -inf).  What lies at positions that no token sees, or that only other tokens
- * see, has no influence (NaN and infinities included).
+ * see, has no influence (NaN and infinities included).  An infinite value makes its dimension infinite, or NaN, for the
+ * tokens that see it.
  *
  *   q         DEVICE rows of n_heads * head_dim values, ldq values from row to row (a multiple of 8), 16-byte aligned; q_dtype = the
  *             cache's type, or AFX_F32 where max_new <= AFX_MAX_T (AFX_ERR_UNSUPPORTED above).

@@ -42,39 +42,72 @@ struct RowState {
     float m = -INFINITY, l = 0.0f, acc[D / 32];
 };
 
-// Positions [from, to) of (sequence b, kv head g) added to the row with query q (times scale * log2 e).
+// Positions [from, to) of (sequence b, kv head g) added to the row with query q (times scale * log2 e), four on their way at
+// once.  Nothing more is added once every sum is infinite or NaN: none becomes finite again.
 template <int D, int CT>
 __device__ __forceinline__ void attend_row(const PagedView& w, int b, int g, const float (&q)[D / 32], int from, int to,
                                            RowState<D>& s) {
-    constexpr int E = D / 32;
+    constexpr int E = D / 32, U = 4;
     const int lane = lane_id();
+    for (int p0 = from; p0 < to; p0 += U) {
+        uint32_t kr[U][E / 2], vr[U][E / 2];
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = p0 + u < to ? paged_row(w, b, p0 + u, g) : -1;
+            in[u] = at >= 0;
+            if (at < 0 && p0 + u < to && lane == 0) report_status(w.status, AFX_ERR_INVALID_ARG);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                kr[u][i] = in[u] ? reinterpret_cast<const uint32_t*>(w.k + at)[lane * (E / 2) + i] : 0u;
+                vr[u][i] = in[u] ? reinterpret_cast<const uint32_t*>(w.v + at)[lane * (E / 2) + i] : 0u;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!in[u]) continue;
+            float d = 0.0f, v[E];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+                const float2 kk = pair_values<CT>(kr[u][i]), vv = pair_values<CT>(vr[u][i]);
+                d = fmaf(q[2 * i], kk.x, d);
+                d = fmaf(q[2 * i + 1], kk.y, d);
+                v[2 * i] = vv.x;
+                v[2 * i + 1] = vv.y;
+            }
+            d = warp_sum(d);
+            const float mn = fmaxf(s.m, d);
+            const float ref = mn == -INFINITY ? 0.0f : mn;
+            const float f = fast_exp2(s.m - ref), pw = fast_exp2(d - ref);
+            s.m = mn;
+            s.l = fmaf(s.l, f, pw);
+#pragma unroll
+            for (int i = 0; i < E; ++i) s.acc[i] = fmaf(s.acc[i], f, pw * v[i]);
+        }
+        if (to - from > U) {
+            bool some = false;
+#pragma unroll
+            for (int i = 0; i < E; ++i) some |= fabsf(s.acc[i]) <= 3.402823466e38f;
+            if (!__any_sync(0xFFFFFFFFu, some)) return;
+        }
+    }
+}
+
+// Whether one of the values at positions [from, to) of (sequence b, kv head g) is infinite or NaN; the same for the warp.
+template <int D, int CT>
+__device__ __forceinline__ bool any_value_not_finite(const PagedView& w, int b, int g, int from, int to) {
+    constexpr int E = D / 32;
+    constexpr uint32_t top = CT == AFX_F16 ? 0x04000400u : 0x00800080u;  // an exponent of ones carries into the sign's place
+    uint32_t found = 0;
+#pragma unroll 4
     for (int p = from; p < to; ++p) {
         const int64_t at = paged_row(w, b, p, g);
-        if (at < 0) {
-            if (lane == 0) report_status(w.status, AFX_ERR_INVALID_ARG);
-            continue;
-        }
-        const uint32_t* kr = reinterpret_cast<const uint32_t*>(w.k + at) + lane * (E / 2);
-        const uint32_t* vr = reinterpret_cast<const uint32_t*>(w.v + at) + lane * (E / 2);
-        float d = 0.0f;
-        float v[E];
+        if (at < 0) continue;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            const float2 kk = pair_values<CT>(kr[i]), vv = pair_values<CT>(vr[i]);
-            d = fmaf(q[2 * i], kk.x, d);
-            d = fmaf(q[2 * i + 1], kk.y, d);
-            v[2 * i] = vv.x;
-            v[2 * i + 1] = vv.y;
-        }
-        d = warp_sum(d);
-        const float mn = fmaxf(s.m, d);
-        const float ref = mn == -INFINITY ? 0.0f : mn;
-        const float f = fast_exp2(s.m - ref), pw = fast_exp2(d - ref);
-        s.m = mn;
-        s.l = fmaf(s.l, f, pw);
-#pragma unroll
-        for (int i = 0; i < E; ++i) s.acc[i] = fmaf(s.acc[i], f, pw * v[i]);
+        for (int i = 0; i < E / 2; ++i)
+            found |= ((reinterpret_cast<const uint32_t*>(w.v + at)[lane_id() * (E / 2) + i] & 0x7FFF7FFFu) + top) & 0x80008000u;
     }
+    return __any_sync(0xFFFFFFFFu, found != 0u);
 }
 
 }  // namespace afx

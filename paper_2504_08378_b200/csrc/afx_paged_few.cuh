@@ -639,6 +639,9 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
             for (int r = 0; r < 8; ++r)
                 if ((lanes >> (4 * r)) & 0xFu) bad |= 1u << (r + 8 * e);
         }
+        // One token sees whatever is read for it: such sums are what they are.  (In 16 rows a weight's two halves meet in one sum, and
+        // their signs may make an infinity NaN: those are taken again.)
+        if (PACK && q.s.n == 1) bad = 0;
         if (tig == 0) {
 #pragma unroll
             for (int e = 0; e < NR; ++e) {

@@ -692,7 +692,21 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 fin &= fabsf(o[c]) <= 3.402823466e38f;
                 o[c] = none ? 0.0f : o[c] * inv;
             }
-            if (live && fin) {
+            // Rows whose sums are not finite.  Where they see what is not finite, that is what they are; but a weight of zero times a NaN or
+            // an infinity that a row does not see has to be nothing.  Only the tiles at the ends of what the rows see hold places that
+            // are masked: if a value there is not finite, the rows are taken again, over what they see alone, on the fp32 pipe.
+            bool again = false;
+            if (__any_sync(0xFFFFFFFFu, live && !fin)) {
+                const uint32_t there = __ballot_sync(0xFFFFFFFFu, live);  // (the warp's rows in front)
+                const int lo = max(__shfl_sync(0xFFFFFFFFu, pos, 0), -1), hi = __shfl_sync(0xFFFFFFFFu, pos, there != 0 ? 31 - __clz(there) : 0);
+                const int back = min(w.end, w.tiles[x] * kPrPos - shift);  // behind the last tile's places
+                again = any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, max(lo + 1, 0), back);
+                if (a.mask.window > 0) {
+                    again |= any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, w.low, min(max(hi - a.mask.window + 1, w.low), w.end));
+                    again |= any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, min(a.mask.sinks, w.few), w.few);
+                }
+            }
+            if (live && (fin || !again)) {
                 uint16_t* dst = a.out + at * D;
                 uint32_t y[D / 2];
 #pragma unroll
@@ -713,11 +727,9 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
 #pragma unroll
                     for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4*>(dst)[c] = *reinterpret_cast<const uint4*>(y + 4 * c);
                 }
-                if (a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;
             }
-            // Rows whose sums are not finite: what they do not see may have been NaN or infinite (a weight of zero times it).
-            // Again, over what the row sees alone, on the fp32 pipe.
-            uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin);
+            if (live && a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;  // (the values have no part in it)
+            uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin && again);
             for (; left != 0; left &= left - 1) {
                 const int who = __ffs(left) - 1;
                 const int wi = __shfl_sync(0xFFFFFFFFu, i, who), wh = __shfl_sync(0xFFFFFFFFu, h, who);
@@ -739,7 +751,6 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     a.out[wat * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
-                if (a.lse != nullptr && lane == 0) a.lse[wat] = st.l == 0.0f ? -INFINITY : (st.m + log2f(st.l)) * kLn2;
             }
         }
         if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);

@@ -345,3 +345,23 @@ def test_thousands_of_sequences_most_of_them_idle(every):
 def test_prompts_beside_decoding_sequences(cache, dim, heads, kv):
     check(Problem([700, 333, 900, 60, 1, 2000, 12], [300, 1, 9, 60, 1, 8, 12], heads, kv, dim, 16, cache, pad=1))
     check(Problem([700, 333, 900, 60, 1, 2000, 12], [300, 1, 9, 60, 1, 8, 12], heads, kv, dim, 48, cache, pad=1), window=100, sinks=5)
+
+
+@pytest.mark.parametrize("heads,kv", [(8, 8), (16, 2), (40, 2)])
+@pytest.mark.parametrize("cache,dim", [("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("lens", [[900], [900, 40]])
+def test_one_token_over_an_infinite_value(heads, kv, cache, dim, lens):
+    p = Problem(lens, [1] * len(lens), heads, kv, dim, 16, cache)
+    rows = p.rows_of(p.both, 0, 1).clone()
+    rows[0, :, 7], rows[700, :, 9] = math.inf, -math.inf
+    p.cells(0, 1)[:] = rows
+    q = p.randn(p.rows, heads, dim, dtype=cache)
+    out, lse = attend(p, q, p.upload(afx), cache, cache)
+    rows[0, :, 7] = rows[700, :, 9] = 0
+    p.cells(0, 1)[:] = rows
+    want, _, mass, norm = p.attend(q)
+    tol = attention_tolerance(want, mass, norm, dim, cache, cache)
+    o = out.double().numpy()
+    assert (o[0, :, 7] == np.inf).all() and (o[0, :, 9] == -np.inf).all() and torch.isfinite(lse).all()
+    o[0][:, [7, 9]] = want[0][:, [7, 9]]
+    assert (np.abs(o - want) <= tol).all()

@@ -246,3 +246,39 @@ def test_prompts_in_a_pool_beyond_32_bits(page, new):
     assert ((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1.1 * 2.0 ** -8 * mass).all()
     del k, v, c
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("cache,dim", [("f16", 128), ("bf16", 64)])
+def test_a_value_that_every_token_sees_spoils_its_dimension_alone(bad, cache, dim):
+    p = Problem(*busy([1300], [1250]), 4, 2, dim, 16, cache)
+    b = p.lens.index(1300)
+    rows = p.rows_of(p.both, b, 1).clone()
+    rows[0, :, 7] = bad
+    p.cells(b, 1)[:] = rows
+    q = p.randn(p.rows, 4, dim, dtype=cache)
+    out, lse = attend(p, q, p.upload(afx), cache, cache)
+    rows[0, :, 7] = 0
+    p.cells(b, 1)[:] = rows
+    want, want_lse, mass, norm = p.attend(q)
+    tol = attention_tolerance(want, mass, norm, dim, cache, cache)
+    o = out.double().numpy()
+    assert not np.isfinite(o[..., 7]).any()
+    rest = [d for d in range(dim) if d != 7]
+    assert (np.abs(o - want)[..., rest] <= tol[..., rest]).all()
+    assert np.abs(lse.double().numpy() - want_lse).max() <= 1e-3
+
+
+def test_prompts_over_a_cache_of_nan_end_soon():
+    """Everything NaN: the rows are taken again, but each ends with its first position."""
+    n = 20000
+    p = Problem([n], [4000], 8, 2, 64, 16, "bf16", filled=False)
+    q = p.randn(p.rows, 8, 64, dtype="bf16")
+    kvd = p.upload(afx)
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.record()
+    out, _ = attend(p, q, kvd, "bf16", "bf16")
+    b.record()
+    torch.cuda.synchronize()
+    assert torch.isnan(out).all()
+    assert a.elapsed_time(b) < 20000  # (some milliseconds; 128000 rows of 20000 positions one after the other would be minutes)
