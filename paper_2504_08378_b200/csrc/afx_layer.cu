@@ -7,6 +7,7 @@
 #include "afx_attn.cuh"
 #include "afx_fused.cuh"
 #include "afx_launch.cuh"
+#include "afx_paged_attn.cuh"
 
 namespace afx {
 
@@ -657,8 +658,8 @@ extern "C" afx_status afx_layer_step_paged(afx_model* m, int layer, afx_state* s
         return afx_paged_append(&c, &prep, q, m->n_qkv, k, m->n_qkv, v, m->n_qkv, rotated, AFX_F32, dev_status, stream);
     };
     auto attend = [&](const afx_paged_kv& c) {
-        return afx_paged_attn(&c, rotated, AFX_F32, ldq, d.n_heads, 0.0f, window, sinks, attn, d.dtype, nullptr, workspace, attn_bytes,
-                              dev_status, stream);
+        return paged_attn(&c, rotated, AFX_F32, ldq, d.n_heads, 0.0f, window, sinks, attn, d.dtype, nullptr, workspace, attn_bytes,
+                          true, dev_status, stream);
     };
     // both calls' checks (without sequences they launch nothing) before anything is enqueued
     afx_paged_kv none = *kv;

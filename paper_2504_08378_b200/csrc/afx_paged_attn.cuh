@@ -19,6 +19,12 @@ struct PagedAttnArgs {
     float* lse;      // or NULL
 };
 
+// afx_paged_attn (afx_paged_attn.cu).  past_final: the kernel in front of it in the stream is the afx_paged_append of the same
+// tokens, and was itself let in by a kernel that waits for all before it.
+afx_status paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads, float scale, int window,
+                      int sinks, void* out, int out_dtype, float* lse, void* workspace, size_t workspace_bytes, bool past_final,
+                      int32_t* dev_status, void* stream);
+
 constexpr float kLn2 = 0.6931471805599453f;
 
 template <int CT>

@@ -69,6 +69,7 @@ struct PagedFewArgs {
     uint32_t rep_mul;    // r / rep = (r * rep_mul) >> 32 for 0 <= r < 2^16 (rep > 1)
     FewJoin* joins;
     float* slots;
+    bool past_final;     // what lies before the new tokens is final since two kernels ago
 };
 
 // Most new tokens of a sequence that these kernels take: AFX_MAX_T, or what makes `groups` groups of 16 rows.  More groups than
@@ -335,10 +336,19 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dyn)) + warp * Cfg::kWarpRing;
 
     if constexpr (ONE) cluster_arrive();
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    // A block of ONE fills its SM.  Were the next kernel let in now, its blocks would all wait on the few SMs without one, and
-    // share them afterwards: a layer step of 4096 x 11008 with 2049 positions took 97 us like that, 75 without.
-    if constexpr (!ONE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    bool waited = false;  // (the same for a warp)
+    auto depend = [&]() {
+        if (waited) return;
+        waited = true;
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        // A block of ONE fills its SM.  Were the next kernel let in now, its blocks would all wait on the few SMs without one,
+        // and share them afterwards: a layer step of 4096 x 11008 with 2049 positions took 97 us like that, 75 without.
+        if constexpr (!ONE) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    };
+    // Inside a layer step the previous kernel is the one that stores the new tokens' rows.  Lengths, table and what lies
+    // before the first new position were there earlier: the first chunks are requested while it runs.  Not for several
+    // sequences: one's past may be another's new token, where they share pages.
+    if (!ONE || !f.past_final) depend();
 
     const int my = blockIdx.x;  // range, or rank in the cluster
     FewWalk con;
@@ -349,6 +359,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         con.q = few_seq(f, 0, blockIdx.x == 0 && blockIdx.y == 0);
         con.item = blockIdx.y;
         if (con.item >= con.q.items) {  // (the same for the cluster)
+            depend();
             cluster_wait();
             return;
         }
@@ -400,22 +411,25 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         int64_t rest;  // what comes to the page's offset
         int page;
         int kind;      // 0: a position, -1: behind the last one, -2: there is no chunk (the same for all lanes)
+        bool fresh;    // a new token's position
     };
     auto look_up = [&]() -> Ahead {
         while (pro.more && pk >= pn) {
             pro.next(f);
             pk = 0;
             pn = pro.more ? pro.chunks<W>(warp) : 0;
-            if (pro.more) warm_queries(pro);
+            if (pro.more) warm_queries(pro);  // (never of ONE, whose blocks have a piece each)
         }
-        Ahead a = {0, 0, -2};
+        Ahead a = {0, 0, -2, false};
         if (!pro.more) return a;
         const int v = ((pro.t0 + pk) * W + warp) * kFewChunk + (lane & 15);
         ++pk;
         a.kind = v < pro.q.nv ? 0 : -1;
         if (a.kind == 0) {
             int in_page;
-            a.page = paged_entry(f.a.w, pro.b, few_pos(pro.q, v), in_page);
+            const int p = few_pos(pro.q, v);
+            a.fresh = p >= pro.q.s.first;
+            a.page = paged_entry(f.a.w, pro.b, p, in_page);
             a.rest = in_page * f.a.w.pos_stride + pro.kv_head * f.a.w.head_stride;
         }
         return a;
@@ -442,7 +456,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (con.more) warm_queries(con);
+    if (waited && con.more) warm_queries(con);
     Ahead ahead;  // the chunk behind those on their way: looked up a chunk's time before it is wanted
     {
         Ahead off[ST - 1];
@@ -450,8 +464,12 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         for (int i = 0; i < ST - 1; ++i) off[i] = look_up();
         ahead = look_up();
 #pragma unroll
-        for (int i = 0; i < ST - 1; ++i) issue(off[i]);
+        for (int i = 0; i < ST - 1; ++i) {
+            if (!waited && __any_sync(0xFFFFFFFFu, off[i].fresh)) depend();
+            issue(off[i]);
+        }
     }
+    depend();
 
     int stage = 0;
     for (; con.more; con.next(f)) {

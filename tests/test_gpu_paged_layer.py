@@ -228,3 +228,62 @@ def test_prompts_chunks_drafts_and_tokens_together(cache, page, dim):
         k64, size = turn(x[b][:, heads:heads + kv], None, 0, cos[pos], sin[pos], "halves")
         assert ((p.rows_of(now, b, 0).double() - k64).abs() <= step * k64.abs() + 2.0 ** -25 + 3.1 * 2.0 ** -24 * size).all()
         assert torch.equal(p.rows_of(now, b, 1), x[b][:, heads + kv:])
+
+
+@pytest.mark.parametrize("news,window,sinks", [(1, 0, 0), (3, 0, 0), (1, 40, 3)])
+def test_one_sequence_runs_on_as_it_goes_step_by_step(news, window, sinks):
+    """Every layer's attention of a single sequence asks for its past before the new rows are stored: the bits are those
+    of steps with the device idle between them."""
+    heads, kvh, n_layers, n_tok, first = 4, 2, 3, 24, 110
+    end = first + n_tok * news
+    states = []
+    for idle in (True, False):
+        m, _ = make("f16", heads, kvh, news, n_layers)
+        probs = [Problem([end], [news], heads, kvh, 128, 16, "f16", seed=l) for l in range(n_layers)]
+        kvs = [p.upload(afx) for p in probs]
+        hs = torch.randn((n_tok, news, m.hidden), generator=torch.Generator().manual_seed(5)).cuda()
+        lens = torch.tensor([first], dtype=torch.int32, device="cuda")
+        outs = torch.zeros((n_tok, news, m.hidden), device="cuda")
+        for t in range(n_tok):
+            lens.add_(news)
+            for p in probs:
+                p.d_len.copy_(lens)
+            m.h.copy_(hs[t])
+            for l in range(n_layers):
+                m.layer_step_paged(l, kvs[l], window, sinks)
+                if idle:
+                    torch.cuda.synchronize()
+            outs[t].copy_(m.h)
+        torch.cuda.synchronize()
+        states.append((outs.clone(), [p.d_both.view(torch.int16).clone() for p in probs]))
+        m.close()
+    assert torch.isfinite(states[0][0]).all()
+    assert torch.equal(states[0][0], states[1][0]) and all(torch.equal(a, b) for a, b in zip(states[0][1], states[1][1]))
+
+
+def test_sequences_that_share_pages_see_each_others_new_tokens():
+    """Tokens of one text as sequences of one token each over the same pages: the second reads what the first stores in
+    the same step.  The same cache as one sequence of two tokens gives the same rows up to the order of its sums."""
+    heads, kvh, n = 4, 2, 150
+    m, _ = make("f16", heads, kvh, 2)
+    p = Problem([n], [2], heads, kvh, 128, 16, "f16", seed=3)
+    one = p.upload(afx)
+    h0 = torch.randn((2, m.hidden), generator=p.g).cuda()
+    start = p.d_both.clone()
+    m.h.copy_(h0)
+    m.layer_step_paged(0, one)
+    want, cache = m.bits(afx.BUF_ATTN).clone().view(torch.float16).double(), p.d_both.clone()
+    two = afx.PagedKV.from_buffer_copy(one)
+    lens = torch.tensor([n - 1, n], dtype=torch.int32, device="cuda")
+    table = p.d_table.repeat(2, 1).contiguous()
+    two.n_seqs, two.max_new, two.tok_start = 2, 1, None
+    two.seq_len, two.page_table, two.table_stride = lens.data_ptr(), table.data_ptr(), table.shape[1]
+    p.d_both.copy_(start)
+    m.h.copy_(h0)
+    m.layer_step_paged(0, two)
+    got = m.bits(afx.BUF_ATTN).view(torch.float16).double()
+    torch.cuda.synchronize()
+    assert torch.equal(cache.view(torch.int16), p.d_both.view(torch.int16))
+    # fp16 rows of values below 8: two roundings of half a step each, and sums of 150 weights in 32 bits
+    assert (got - want).abs().max() <= 2 * 2.0 ** -11 * 8
+    m.close()
