@@ -691,7 +691,8 @@ afx_status afx_mlp_block_noalloc(const void* w_gu, const void* w_down, int dtype
  * left out (AFX_ERR_CAPACITY); a position whose page id is outside [0, n_pages), or that is negative
  * (more new tokens than positions), is not written and not attended to (AFX_ERR_INVALID_ARG).
  * Entries of the table that no token of the call sees (pages behind a sequence's end, or in front of every token's window) are not
- * looked at.  Two tokens of a call must not share a cache row, nor two sequences a page that one of them writes.  All
+ * looked at.  Two tokens of a call must not share a cache row, nor a new token one that an earlier position of its sequence
+ * is still seen in.  Sequences may share pages: attention sees what was appended before it, by whichever of them.  All
  * buffers belong to the current device.
  * ------------------------------------------------------------------------------------------ */
 
