@@ -207,6 +207,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     __shared__ __align__(16) uint4 answer;  // of the request for the next block
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
+    __shared__ int steps[kPrLoaders];  // of the ring, that each of the loading warps has made in the end
     __shared__ PrWork work[2];
     __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -367,10 +368,9 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 }
             }
             if (!ok && lead) {  // what has been issued ends before tensor memory is given back
-                int alone = 0;
                 report_status(a.w.status, AFX_ERR_TIMEOUT);
                 tc_commit(&bar.drain);
-                mbar_wait(&bar.drain, 0, &alone);
+                mbar_drain(&bar.drain, 0);
             }
             __syncwarp();
         } else {
@@ -522,7 +522,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     if (lw == 2 && j == min(2, n_tiles - 1)) {
                         // the next work, as soon as this one's first tiles are on their way
                         ok = wait(&bar.answered, it & 1);
-                        asked = 0;
+                        if (ok) asked = 0;
                         const int place = ok ? clc_place(&answer) : -1;
                         fence_proxy_async();
                         if (ok && it >= 1) ok = wait(&bar.work_empty[(it + 1) & 1], (((it + 1) >> 1) & 1) ^ 1);
@@ -539,11 +539,9 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (!ok) {
                 if (lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
-                if (asked > 0) {  // the answer is written before the block ends
-                    int alone = 0;
-                    mbar_wait(&bar.answered, (asked - 1) & 1, &alone);
-                }
+                if (asked > 0) mbar_drain(&bar.answered, (asked - 1) & 1);  // the answer is written before the block ends
             }
+            if (lane == 0) steps[lw] = static_cast<int>(turn) * NB + slot;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPrRowRegs));
@@ -759,6 +757,14 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    if (gave_up != 0 && warp > 8) {
+        // Boxes may be under way yet.  A slot's phase ends when its boxes are there and all three warps have arrived; one that gave
+        // up owes arrivals for the steps that another has made (fewer than the ring has slots: a slot is filled again after all have
+        // arrived for its step before), and makes them now.
+        const int all = max(max(steps[0], steps[1]), steps[2]);
+        for (int i = steps[warp - 9]; i < all; ++i) mbar_arrive(&bar.full[i % NB]);
+        for (int i = max(all - NB, 0); i < all; ++i) mbar_drain(&bar.full[i % NB], (i / NB) & 1);
+    }
     if (warp == 8) tmem_free(tmem, 512);
 }
 

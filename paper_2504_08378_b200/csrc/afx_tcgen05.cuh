@@ -41,22 +41,35 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
         : "memory");
     return done != 0;
 }
+// Nanoseconds that a wait lasts at most (a build for tests may say otherwise).
+#ifndef AFX_WAIT_NS
+#define AFX_WAIT_NS 2000000000ull
+#endif
 // Waits for the phase of that parity, but not for ever: false after two seconds, which no wait of a working kernel comes
 // near, or when another waiter of the block has given up.  *gave_up is the block's flag in shared memory.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* gave_up) {
     uint64_t t0 = 0;
-    for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
-        if ((i & 255u) != 0) continue;
+    while (!mbar_try_wait(bar, parity)) {
         uint64_t t;
         asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
         if (t0 == 0) t0 = t;
         if (*gave_up != 0) return false;
-        if (t - t0 > 2000000000ull) {
+        if (t - t0 > AFX_WAIT_NS) {
             *gave_up = 1;
             return false;
         }
     }
     return true;
+}
+// The wait of a thread that has given up for what it still has under way, which comes in any case: two seconds whatever the limit above.
+__device__ __forceinline__ void mbar_drain(uint64_t* bar, uint32_t parity) {
+    uint64_t t0 = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        uint64_t t;
+        asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+        if (t0 == 0) t0 = t;
+        if (t - t0 > 2000000000ull) return;
+    }
 }
 
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
