@@ -37,6 +37,10 @@ constexpr int kPrLoaders = 3;
 // Registers of a thread of the loading and issuing warps, and of the rows' warps: 128 and 256 threads share the 384 x 168 of the launch.
 constexpr int kPrLoadRegs = 104, kPrRowRegs = 200;
 static_assert(128 * kPrLoadRegs + 256 * kPrRowRegs <= kPrThreads * 168, "more than the launch has");
+// Positions after which a warp that takes a row again says so (0.3 ms; a build for tests may say otherwise).
+#ifndef AFX_TELL_EVERY
+#define AFX_TELL_EVERY 1024
+#endif
 constexpr float kPrGrow = 8.0f;  // powers of two that a row's maximum may grow by before O is rescaled
 
 struct PagedPromptArgs {
@@ -206,7 +210,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     __shared__ PrBarriers bar;
     __shared__ __align__(16) uint4 answer;  // of the request for the next block
     __shared__ uint32_t tmem_at;
-    __shared__ int gave_up;
+    __shared__ Patience patience;
     __shared__ int steps[kPrLoaders];  // of the ring, that each of the loading warps has made in the end
     __shared__ PrWork work[2];
     __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
@@ -215,7 +219,8 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     const uint32_t base = smem_u32(dyn);
 
     if (tid == 0) {
-        gave_up = 0;
+        patience.gave_up = 0;
+        patience.told = nanoseconds();
         mbar_init(&bar.q_full, kPrLoaders * 32);
         mbar_init(&bar.q_empty, 1);
         for (int i = 0; i < NB; ++i) {
@@ -255,7 +260,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
 
     // A warp's next work (in its registers), the same for the whole warp; b < 0: there is none.  it counts the block's works.
     auto next_work = [&](int it, PrWork& w) {
-        const bool in = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.work_full[it & 1], (it >> 1) & 1, &gave_up));
+        const bool in = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.work_full[it & 1], (it >> 1) & 1, &patience));
         if (in) {
             w = work[it & 1];
             __syncwarp();
@@ -273,7 +278,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             constexpr uint32_t o_desc = mma_desc(CT == AFX_BF16, 128, D, true);
             const bool lead = elect_one();
             const uint32_t tm = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
+            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &patience)) != 0; };
             // The ring's tiles in the order of their use (K0, V0, K1, V1, ..).  The loaders' copies of rows are writes like any thread's,
             // the products read shared memory by another path: the fence stands between what the barrier says and them.
             int slot = 0;
@@ -384,7 +389,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             auto when_landed = [&](uint64_t* full) {  // an arrival of this thread's as soon as its copies so far have landed
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full)) : "memory");
             };
-            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &gave_up)) != 0; };
+            auto wait = [&](uint64_t* b, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(b, parity, &patience)) != 0; };
             const int boxes = kPrPos / args.box;
             // the ring's next slot: its tile before has been used (after the first turn)
             int slot = 0, ok_slot = 0;
@@ -572,7 +577,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             const int lo_all = a.mask.window > 0 ? w.first + max(rr1, 0) / a.rep - a.mask.window + 1 + shift : 0;
             float m = -INFINITY, l = 0.0f;
             for (int j = 0; ok && j < w.tiles[x]; ++j) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.s_full[x], s_turn, &gave_up));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.s_full[x], s_turn, &patience));
                 s_turn ^= 1u;
                 if (!ok) break;
                 tc_fence_after();
@@ -665,7 +670,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             if (!ok) break;
             ok_slot = (ok_slot + max(w.tiles[0], w.tiles[1])) & 7;
             if (w.tiles[x] > 0) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.o_full[x], o_turn, &gave_up));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&bar.o_full[x], o_turn, &patience));
                 o_turn ^= 1u;
                 if (!ok) break;
                 tc_fence_after();
@@ -740,10 +745,15 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     st.acc[e] = 0.0f;
                     q[e] = a.scale * typed_value(a.q, a.q_type, (w.row0 + wi) * a.ldq + static_cast<int64_t>(wh) * D + lane * E + e);
                 }
-                if (wp >= 0) {
-                    const int low = paged_low(a.mask, wp);
-                    attend_row<D, CT>(a.w, w.b, w.kv_head, q, 0, paged_few(a.mask, low), st);
-                    attend_row<D, CT>(a.w, w.b, w.kv_head, q, low, wp + 1, st);
+                // (This may take long, and the block's other warps wait for it with the next work: they are told that it goes on.)
+                const int low = paged_low(a.mask, wp), few = paged_few(a.mask, low);
+                for (int part = 0; wp >= 0 && part < 2; ++part) {
+                    const int end = part == 0 ? few : wp + 1;
+                    for (int from = part == 0 ? 0 : low, to; from < end; from = to) {
+                        to = end - from > AFX_TELL_EVERY ? from + AFX_TELL_EVERY : end;
+                        attend_row<D, CT>(a.w, w.b, w.kv_head, q, from, to, st);
+                        if (lane == 0) *const_cast<volatile uint32_t*>(&patience.told) = nanoseconds();
+                    }
                 }
                 const int64_t wat = static_cast<int64_t>(w.row0 + wi) * a.heads + wh;
 #pragma unroll
@@ -757,7 +767,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (gave_up != 0 && warp > 8) {
+    if (patience.gave_up != 0 && warp > 8) {
         // Boxes may be under way yet.  A slot's phase ends when its boxes are there and all three warps have arrived; one that gave
         // up owes arrivals for the steps that another has made (fewer than the ring has slots: a slot is filled again after all have
         // arrived for its step before), and makes them now.

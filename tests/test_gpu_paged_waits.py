@@ -69,3 +69,35 @@ def test_a_wait_that_runs_out_is_reported_and_the_gpu_goes_on(waits, page):
     assert (stayed | same).all()
     again, status = run(waits, p, q, kvd, 2 * 10 ** 9)
     assert status == 0 and torch.equal(again.view(torch.int16), whole.view(torch.int16))
+
+
+def test_rows_that_are_taken_again_keep_the_others_waiting(waits):
+    """The first sequence's rows are taken again for longer than the limit, while blocks hold works of the other sequences:
+    nobody gives up, and every row is right."""
+    p = problem(64)
+    q = p.randn(p.rows, HEADS, DIM, dtype="bf16").cuda()
+    kvd = p.upload(afx)
+    whole, _ = attend(p, q.cpu(), kvd, "bf16", "bf16")
+    try:
+        assert waits.waits_tell_every(1024) == 0
+        out, status = run(waits, p, q, kvd, 5 * 10 ** 6)
+    finally:
+        assert waits.waits_tell_every(0x7FFFFFFF) == 0
+    assert status == 0
+    assert torch.equal(out.view(torch.int16), whole.view(torch.int16))
+    # the rows in front of the infinite value, and those of the other sequences, by the definition
+    rows = p.rows_of(p.both, 0, 1).clone()
+    rows[-1, :, 5] = 0
+    p.cells(0, 1)[:] = rows
+    some = [0, 300, 505, 510]
+    K, V = (p.rows_of(p.both, 0, c).double() for c in (0, 1))
+    for i in some:
+        pos = 40000 - 512 + i
+        for h in (0, 5, 31):
+            k, v = K[:pos + 1, h // 4], V[:pos + 1, h // 4]
+            s = k @ q[i, h].double().cpu() / 8
+            w = torch.softmax(s, 0)
+            size = (k.abs() @ q[i, h].double().cpu().abs()).max().item() / 8
+            tol = attention_tolerance((w @ v).numpy(), (w @ v.abs()).numpy(), np.float64(size), DIM, "bf16", "bf16")
+            assert (np.abs(out[i, h].double().numpy() - (w @ v).numpy()) <= tol).all()
+    assert torch.isposinf(out[511, :, 5]).all() and torch.isfinite(out[:511]).all() and torch.isfinite(out[512:]).all()

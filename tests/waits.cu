@@ -1,6 +1,9 @@
 // The prompts' attention built with a limit of its waits that a test sets (test_gpu_paged_waits.py).
+// Rows that are taken again say so after tell_every positions: never, unless the test says otherwise.
 static __device__ unsigned long long limit_ns;
+static __device__ int tell_every = 0x7FFFFFFF;
 #define AFX_WAIT_NS limit_ns
+#define AFX_TELL_EVERY tell_every
 #include "afx_paged_prompt.cu"
 #include "afx_paged.cu"
 
@@ -12,6 +15,8 @@ int afx::sm_count() {
 }
 
 extern "C" int waits_limit(unsigned long long ns) { return static_cast<int>(cudaMemcpyToSymbol(limit_ns, &ns, sizeof ns)); }
+
+extern "C" int waits_tell_every(int positions) { return static_cast<int>(cudaMemcpyToSymbol(tell_every, &positions, sizeof positions)); }
 
 // afx_paged_attn of every sequence by tiles, out in the cache's type
 extern "C" int waits_prompt(const afx_paged_kv* kv, const void* q, int64_t ldq, int n_heads, void* out, float* lse, int32_t* dev_status) {
