@@ -686,7 +686,7 @@ afx_status afx_mlp_block_noalloc(const void* w_gu, const void* w_down, int dtype
  *     page_table[b * table_stride + p / page_size] * page_stride + (p % page_size) * pos_stride + g * head_stride + d
  * of k_pages and of v_pages (position-major and head-major pages, K and V in one buffer or in two).
  * Lengths, starts and page ids are device data and checked there (dev_status): a length outside
- * [0, table_stride * page_size] is clamped (AFX_ERR_CAPACITY), a start outside [start before, n_tokens]
+ * [0, table_stride * page_size] is clamped (AFX_ERR_CAPACITY), a start outside [largest start before, n_tokens]
  * likewise (AFX_ERR_INVALID_ARG); of a sequence with more than max_new new tokens the rows behind the first max_new are
  * left out (AFX_ERR_CAPACITY); a position whose page id is outside [0, n_pages), or that is negative
  * (more new tokens than positions), is not written and not attended to (AFX_ERR_INVALID_ARG).

@@ -115,6 +115,7 @@ template <int D, int XT>
 __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(AppendArgs a) {
     constexpr int GL = D / 16, RPP = kAppendThreads / GL, XB = XT == AFX_F32 ? 4 : 2;
     __shared__ float4 rot[2][D / 8];  // of the token's position
+    __shared__ int found[2][kAppendThreads / 32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int t = blockIdx.x, l = threadIdx.x % GL;
@@ -144,22 +145,42 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(AppendArgs a)
         load_piece<XT>(na, row_of(r), pa);
         load_piece<XT>(nb, row_of(r), pb);
     }
-    int b = t;
-    if (a.w.start != nullptr) {  // the last sequence that starts at or before t
-        b = -1;
-        for (int i = 0; i < a.w.n_seqs + 1; i += kAppendThreads) {
-            const int s = i + static_cast<int>(threadIdx.x);
-            b += __syncthreads_count(s <= a.w.n_seqs && a.w.start[s <= a.w.n_seqs ? s : 0] <= t);
+    int b = t, row0 = t;
+    if (a.w.start != nullptr) {  // the sequence in front of the first one that starts behind t
+        const int n = a.w.n_seqs;
+        int i = 0, upto = 0, lower = 0;  // of 256 starts: how many are at or before t, is one below the one before it
+        for (; i <= n; i += kAppendThreads) {
+            const int x = i + static_cast<int>(threadIdx.x), at = x <= n ? a.w.start[x] : 0x7FFFFFFF;
+            const int before = x > 0 && x <= n ? a.w.start[x - 1] : at;
+            const uint32_t in = __ballot_sync(0xFFFFFFFFu, x <= n && at <= t), down = __ballot_sync(0xFFFFFFFFu, at < before);
+            int* mine = found[(i / kAppendThreads) & 1];
+            if (lane_id() == 0) mine[warp_id()] = __popc(in) + (down != 0 ? 1 << 16 : 0);
+            __syncthreads();
+            upto = 0;
+#pragma unroll
+            for (int w = 0; w < kAppendThreads / 32; ++w) upto += mine[w];
+            lower = upto >> 16;
+            upto &= 0xFFFF;
+            if (lower != 0 || upto < kAppendThreads) break;
+        }
+        if (i > n) return;  // behind the last sequence's rows
+        if (lower == 0) {
+            b = i + upto - 1;
+            row0 = paged_first_row(a.w, max(b, 0));
+        } else {
+            row0 = 0;
+            for (b = -1; b < n; ++b) {
+                const int s = a.w.start[b + 1];
+                if (s > t) break;
+                row0 = max(row0, s);
+            }
         }
     }
     if (b < 0 || b >= a.w.n_seqs) return;  // in front of the first sequence's rows or behind the last one's
     const bool lead = threadIdx.x == 0 && blockIdx.y == 0;
-    const SeqSpan s = paged_span(a.w, b, lead);
+    const SeqSpan s = paged_span(a.w, b, row0, lead);
     const int i = t - s.row0;
-    if (i < 0 || i >= s.n) {
-        if (lead && i < 0) report_status(a.w.status, AFX_ERR_INVALID_ARG);
-        return;
-    }
+    if (i >= s.n) return;  // (reported above)
     const int pos = s.first + i;
     if (pos < 0) return;  // (reported above)
     if (a.half > 0 && pos >= a.rope_len) {

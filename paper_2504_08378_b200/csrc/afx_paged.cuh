@@ -30,26 +30,29 @@ struct SeqSpan {
     int n;      // rows taken part in (at most max_new)
     int first;  // position of row0 (negative: more new tokens than positions)
     int len;    // positions of the cache
+    int next;   // first token row of the next sequence
 };
 
 // Host: checks the descriptor and fills the view.  AFX_OK with n_seqs = 0 or n_tokens = 0: nothing to do.
 afx_status paged_view(const afx_paged_kv* kv, int32_t* dev_status, PagedView* out);  // afx_paged.cu
 
-__device__ __forceinline__ SeqSpan paged_span(const PagedView& w, int b, bool report) {
+// A sequence's rows begin at the largest start so far (starts that decrease are clamped to it): at start[b] where none
+// decreases, and where the sequence before it ends (next) in any case.
+__device__ __forceinline__ int paged_first_row(const PagedView& w, int b) {
+    return w.start != nullptr ? min(max(w.start[b], 0), w.n_tokens) : b;
+}
+__device__ __forceinline__ SeqSpan paged_span(const PagedView& w, int b, int row0, bool report) {
     SeqSpan s;
-    int len = w.len[b], lo = b, hi = b + 1;
-    if (w.start != nullptr) {
-        lo = w.start[b];
-        hi = w.start[b + 1];
-    }
-    const int row0 = min(max(lo, 0), w.n_tokens), row1 = min(max(hi, row0), w.n_tokens);
+    const int len = w.len[b], hi = w.start != nullptr ? w.start[b + 1] : b + 1;
+    const int row1 = min(max(hi, row0), w.n_tokens);
     s.len = min(max(len, 0), w.cap);
     s.row0 = row0;
+    s.next = row1;
     s.first = s.len - (row1 - row0);
     s.n = min(row1 - row0, w.max_new);
     if (report) {
         if (s.len != len) report_status(w.status, AFX_ERR_CAPACITY);
-        if (row0 != lo || row1 != hi || s.first < 0) report_status(w.status, AFX_ERR_INVALID_ARG);
+        if ((w.start != nullptr && w.start[b] != row0) || row1 != hi || s.first < 0) report_status(w.status, AFX_ERR_INVALID_ARG);
         if (s.n != row1 - row0) report_status(w.status, AFX_ERR_CAPACITY);
     }
     return s;

@@ -94,9 +94,9 @@ struct FewSeq {
     int groups;        // row groups
 };
 
-__device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, bool report) {
+__device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, int row0, bool report) {
     FewSeq q;
-    q.s = paged_span(f.a.w, b, report);
+    q.s = paged_span(f.a.w, b, row0, report);
     if (q.s.n > f.most) q.s.n = 0;
     const int first = max(q.s.first, 0), end = min(q.s.len, q.s.first + q.s.n);
     q.low = paged_low(f.a.mask, first);
@@ -125,24 +125,34 @@ struct FewScratch {
     FewStart start;
 };
 // The list's length.  All threads of the block call it.
-// (last: the last of this thread's sequences)
-__device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* sc, bool report, int64_t& mine_before, int64_t& mine,
+// (row0: first token row of this thread's first sequence; last: the last of its sequences)
+__device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* sc, bool report, int& row0, int64_t& mine_before, int64_t& mine,
                                             FewSeq& last) {
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads, tid = threadIdx.x;
-    mine = 0;
-    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
-        const FewSeq q = few_seq(f, i, report);
-        last = q;
-        mine += static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
-    }
-    int64_t incl = mine;
+    const int i0 = min(tid * per, n), i1 = min(n, i0 + per);
+    row0 = paged_first_row(f.a.w, i0);
+    int64_t incl;
+    for (bool again = false;; again = true) {
+        int at = row0;
+        bool down = false;  // a start is below the one before it
+        mine = 0;
+        for (int i = i0; i < i1; ++i) {
+            const FewSeq q = few_seq(f, i, at, report);
+            last = q;
+            mine += static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
+            at = q.s.next;
+            down |= f.a.w.start != nullptr && f.a.w.start[i + 1] < f.a.w.start[i];
+        }
+        incl = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane_id() >= o) incl += up;
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane_id() >= o) incl += up;
+        }
+        if (lane_id() == 31) sc->warp_units[warp_id()] = incl;
+        if (!__syncthreads_or(down) || again) break;
+        for (int i = 0; i <= i0; ++i) row0 = max(row0, paged_first_row(f.a.w, i));
     }
-    if (lane_id() == 31) sc->warp_units[warp_id()] = incl;
-    __syncthreads();
     int64_t total = 0;
     mine_before = incl - mine;
 #pragma unroll
@@ -153,7 +163,7 @@ __device__ __forceinline__ int64_t few_list(const PagedFewArgs& f, FewScratch* s
     return total;
 }
 // The thread among whose sequences unit `at` lies writes down which.
-__device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int64_t mine_before, int64_t mine,
+__device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, int64_t at, int row0, int64_t mine_before, int64_t mine,
                                          const FewSeq& last) {
     if (at < mine_before || at >= mine_before + mine) return;
     const int n = f.a.w.n_seqs, per = (n + kFewThreads - 1) / kFewThreads;
@@ -162,8 +172,9 @@ __device__ __forceinline__ void few_find(const PagedFewArgs& f, FewScratch* sc, 
         return;
     }
     for (int b = threadIdx.x * per; b < min(n, static_cast<int>(threadIdx.x + 1) * per); ++b) {
-        const FewSeq q = few_seq(f, b, false);
+        const FewSeq q = few_seq(f, b, row0, false);
         const int64_t t = static_cast<int64_t>(q.tiles + kFewItemCost) * q.items;
+        row0 = q.s.next;
         if (mine_before + t > at) {
             sc->start = {mine_before, q, b};
             break;
@@ -223,7 +234,7 @@ struct FewWalk {
                         more = false;
                         return;
                     }
-                    q = few_seq(f, b, false);
+                    q = few_seq(f, b, q.s.next, false);
                 } while (q.items == 0);
             }
         } while (!cut(0));
@@ -356,7 +367,7 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
     int64_t hi = 0;
     if constexpr (ONE) {
         con.b = 0;
-        con.q = few_seq(f, 0, blockIdx.x == 0 && blockIdx.y == 0);
+        con.q = few_seq(f, 0, paged_first_row(f.a.w, 0), blockIdx.x == 0 && blockIdx.y == 0);
         con.item = blockIdx.y;
         if (con.item >= con.q.items) {  // (the same for the cluster)
             depend();
@@ -371,15 +382,16 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         con.left = 0;
         con.more = true;
     } else {
+        int row0;
         int64_t mine_before, mine;
         FewSeq last;
-        const int64_t total = few_list(f, &scratch, blockIdx.x == 0, mine_before, mine, last);
+        const int64_t total = few_list(f, &scratch, blockIdx.x == 0, row0, mine_before, mine, last);
         ranges = FewRanges(total, gridDim.x);
         if (tid == 0) f.joins[my].last = -1;  // (a later piece may say otherwise)
         if (my >= ranges.n) return;
         const int64_t lo = ranges.begin(my);
         hi = ranges.begin(my + 1);
-        few_find(f, &scratch, lo, mine_before, mine, last);
+        few_find(f, &scratch, lo, row0, mine_before, mine, last);
         __syncthreads();
         con.b = scratch.start.b;
         con.q = scratch.start.q;
