@@ -139,12 +139,17 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(AppendArgs a)
              : rr < nq + kv ? a.k + (t * a.ldk + static_cast<int64_t>(rr - nq) * D) * XB
                             : a.v + (t * a.ldv + static_cast<int64_t>(rr - nq - kv) * D) * XB;
     };
-    // the first rows are on their way while the token's sequence is looked up
+    // The first rows are on their way while the token's sequence is looked up; not those that no sequence has: they may not be there.
+    const int n0 = a.w.start != nullptr ? a.w.start[0] : 0, n1 = a.w.start != nullptr ? a.w.start[a.w.n_seqs] : a.w.n_seqs;
+    const bool early = t >= n0 && t < n1;
     Piece<XT> na, nb;
-    if (r < r_end) {
-        load_piece<XT>(na, row_of(r), pa);
-        load_piece<XT>(nb, row_of(r), pb);
-    }
+    auto first_rows = [&]() {
+        if (r < r_end) {
+            load_piece<XT>(na, row_of(r), pa);
+            load_piece<XT>(nb, row_of(r), pb);
+        }
+    };
+    if (early) first_rows();
     int b = t, row0 = t;
     if (a.w.start != nullptr) {  // the sequence in front of the first one that starts behind t
         const int n = a.w.n_seqs;
@@ -177,6 +182,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(AppendArgs a)
         }
     }
     if (b < 0 || b >= a.w.n_seqs) return;  // in front of the first sequence's rows or behind the last one's
+    if (!early) first_rows();  // (starts that decrease)
     const bool lead = threadIdx.x == 0 && blockIdx.y == 0;
     const SeqSpan s = paged_span(a.w, b, row0, lead);
     const int i = t - s.row0;

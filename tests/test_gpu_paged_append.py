@@ -247,3 +247,28 @@ def test_buffers_that_begin_on_any_16_bytes():
         torch.cuda.synchronize()
         outs.append((p.d_both.clone().view(torch.int16), q_out.clone()))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and outs[0][1].any()
+
+
+@pytest.mark.parametrize("start", [True, False])
+def test_rows_that_no_sequence_has_need_not_exist(start):
+    """A batch padded far behind the live rows (and, with starts, begun behind its first ones): q, k, v and q_out hold the
+    live rows alone."""
+    H, kv, D, live, front = 8, 2, 128, 3, 4 if start else 0
+    p = Problem([20, 7, 33], [1, 1, 1], H, kv, D, 16, "f16")
+    src = p.randn(live, (H + 2 * kv) * D, dtype="f16").cuda()
+    w = (H + 2 * kv) * D
+    prep = afx.HeadPrep(x_dtype=afx.F16, n_heads=H, eps=1e-5)
+    kvd = p.upload(afx, start=start)
+    if start:
+        p.d_start += front
+    kvd.n_tokens = 100000
+    q_out = torch.zeros((live, H * D), dtype=torch.float16, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    row = lambda t, first: t.data_ptr() + first * 2 - front * t.stride(0) * 2  # where row 0 would be
+    afx.afx_paged_append(kvd, prep, row(src, 0), w, row(src, H * D), w, row(src, (H + kv) * D), w, row(q_out, 0), "f16", dev_status=status)
+    torch.cuda.synchronize()
+    assert status.item() == 0 and torch.equal(q_out, src[:, :H * D])
+    for b, n in enumerate(p.lens):
+        page, slot = p.table[b, (n - 1) // 16].item(), (n - 1) % 16
+        got = p.d_both[page, :, slot].cpu()
+        assert torch.equal(got.reshape(-1), src[b, H * D:].cpu())
