@@ -42,6 +42,16 @@ __device__ __forceinline__ uint16_t typed_bits(float v, int type) {
     return type == AFX_F16 ? float_to_bits<AFX_F16>(v) : float_to_bits<AFX_BF16>(v);
 }
 
+// The sign's places of the halves that are infinite or NaN.  (An exponent of ones carries there.)
+template <int CT>
+__device__ __forceinline__ uint32_t not_finite(uint32_t pair) {
+    return ((pair & 0x7FFF7FFFu) + (CT == AFX_F16 ? 0x04000400u : 0x00800080u)) & 0x80008000u;
+}
+template <int CT>
+__device__ __forceinline__ uint32_t not_finite(const uint4& x) {
+    return not_finite<CT>(x.x) | not_finite<CT>(x.y) | not_finite<CT>(x.z) | not_finite<CT>(x.w);
+}
+
 // Running softmax of one row in a warp: a lane owns D / 32 neighbouring dims.
 template <int D>
 struct RowState {
@@ -103,7 +113,6 @@ __device__ __forceinline__ void attend_row(const PagedView& w, int b, int g, con
 template <int D, int CT>
 __device__ __forceinline__ bool any_value_not_finite(const PagedView& w, int b, int g, int from, int to) {
     constexpr int E = D / 32;
-    constexpr uint32_t top = CT == AFX_F16 ? 0x04000400u : 0x00800080u;  // an exponent of ones carries into the sign's place
     uint32_t found = 0;
 #pragma unroll 4
     for (int p = from; p < to; ++p) {
@@ -111,7 +120,7 @@ __device__ __forceinline__ bool any_value_not_finite(const PagedView& w, int b, 
         if (at < 0) continue;
 #pragma unroll
         for (int i = 0; i < E / 2; ++i)
-            found |= ((reinterpret_cast<const uint32_t*>(w.v + at)[lane_id() * (E / 2) + i] & 0x7FFF7FFFu) + top) & 0x80008000u;
+            found |= not_finite<CT>(reinterpret_cast<const uint32_t*>(w.v + at)[lane_id() * (E / 2) + i]);
     }
     return __any_sync(0xFFFFFFFFu, found != 0u);
 }

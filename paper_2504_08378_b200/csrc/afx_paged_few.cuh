@@ -310,6 +310,57 @@ __device__ __forceinline__ int few_place(int r, int d) {
     return r * DW + (d ^ ((r & 7) << 3));
 }
 
+// Sums that are NaN (of rows `bad`, 64 dims, a lane's two at a time) where the values that are not finite and that the row sees add up
+// to something else: these are the sum.  One pass over the piece's values for all rows; it ends when what is left is NaN.
+template <int D, int CT, int W>
+__device__ __forceinline__ void few_infinite(const PagedFewArgs& f, const FewWalk& c, int warp, uint32_t bad, int part, float* sums) {
+    const int lane = lane_id(), n_chunks = c.chunks<W>(warp);
+    uint32_t open[2] = {0, 0}, hit[2] = {0, 0};  // rows with a NaN in the lane's first and second dim, and those where a value was found
+    for (uint32_t left = bad; left != 0; left &= left - 1) {
+        const int r = __ffs(left) - 1;
+        float* s = sums + few_place<64>(r, 2 * lane);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+            if (s[x] != s[x]) {
+                open[x] |= 1u << r;
+                s[x] = 0.0f;
+            }
+    }
+    for (int k = 0; k < n_chunks && __any_sync(0xFFFFFFFFu, (open[0] | open[1]) != 0u); ++k) {
+        const int v0 = ((c.t0 + k) * W + warp) * kFewChunk, n = min(kFewChunk, c.q.nv - v0);
+        const int64_t mine = lane < n ? paged_row(f.a.w, c.b, few_pos(c.q, v0 + lane), c.kv_head) : -1;
+        uint32_t raw[kFewChunk];
+#pragma unroll
+        for (int j = 0; j < kFewChunk; ++j) {
+            const int64_t at = __shfl_sync(0xFFFFFFFFu, mine, j);
+            raw[j] = at >= 0 ? reinterpret_cast<const uint32_t*>(f.a.w.v + at + part * 64)[lane] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < kFewChunk; ++j) {
+            if (not_finite<CT>(raw[j]) == 0u) continue;
+            const float2 v = pair_values<CT>(raw[j]);
+            const int p = few_pos(c.q, v0 + j);
+            for (uint32_t left = open[0] | open[1]; left != 0; left &= left - 1) {
+                const int r = __ffs(left) - 1;
+                const FewRow fr = few_row(f, c.q, c.kv_head, c.group, r);
+                if (!fr.live || !few_sees(f.a.mask, fr.pos, p)) continue;
+                float* s = sums + few_place<64>(r, 2 * lane);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float value = x == 0 ? v.x : v.y;
+                    if (!((open[x] >> r) & 1u) || fabsf(value) <= 3.402823466e38f) continue;
+                    s[x] += value;
+                    hit[x] |= 1u << r;
+                    if (s[x] != s[x]) open[x] &= ~(1u << r);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        for (uint32_t left = open[x] & ~hit[x]; left != 0; left &= left - 1) sums[few_place<64>(__ffs(left) - 1, 2 * lane) + x] = NAN;
+}
+
 // Four dims of a finished row; nothing seen: zeros.
 template <int D>
 __device__ __forceinline__ void few_store(const PagedFewArgs& f, int t, int h, int d, const float4& s, float M, float L) {
@@ -630,6 +681,41 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                     few_split<CT>(p[2], p[3], pa[2 + e], pl[2 + e]);
                 }
             }
+            // A weight of zero times an infinity or a NaN that its row does not see has to be nothing: in a chunk that not every row sees
+            // such values are added to the rows that see them and are zeros for the product.  (One token sees all that is read.)
+            if (!all && q.s.n > 1) {
+                uint4* vs = reinterpret_cast<uint4*>(dyn + warp * Cfg::kWarpRing + stage * Cfg::kChunkBytes + kFewChunk * D * 2);
+                uint32_t found = 0;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) found |= not_finite<CT>(vs[i * 32 + lane]);
+                if (__any_sync(0xFFFFFFFFu, found != 0u)) {
+#pragma unroll 1
+                    for (int j = 0; j < kFewChunk; ++j) {
+                        const int p = few_pos(q, v0 + j);
+                        const uint32_t* at = reinterpret_cast<const uint32_t*>(vs + j * PIECES) + tig;
+#pragma unroll
+                        for (int e = 0; e < NR; ++e) {
+                            if (!((vm >> j) & 1u) || !few_sees(f.a.mask, pos[e], p)) continue;
+#pragma unroll
+                            for (int i = 0; i < NT; ++i) {
+                                const float2 v = pair_values<CT>(at[(i ^ (j & 7)) * 4]);
+                                if (!(fabsf(v.x) <= 3.402823466e38f)) o[i][2 * e] += v.x;
+                                if (!(fabsf(v.y) <= 3.402823466e38f)) o[i][2 * e + 1] += v.y;
+                            }
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll 1
+                    for (int i = 0; i < D / 16; ++i) {
+                        uint4 x = vs[i * 32 + lane];
+                        uint32_t* w = &x.x;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) w[c] &= ~((not_finite<CT>(w[c]) >> 15) * 0xFFFFu);
+                        vs[i * 32 + lane] = x;
+                    }
+                    __syncwarp();
+                }
+            }
             {
                 const int row = (lane & 7) + (lane & 8), half = lane >> 4;
 #pragma unroll
@@ -651,12 +737,12 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
         }
 
         // ---- the warps' sums meet
-        uint32_t bad = 0;  // rows whose sums are not finite: a value that the row does not see may have been NaN or infinite
+        uint32_t bad = 0;  // rows with sums that are NaN: in 16 rows the signs of a weight's two halves may make an infinity that they see one
 #pragma unroll
         for (int e = 0; e < NR; ++e) {
             l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 1);
             l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 2);
-            bool fin = true;
+            bool nan = false;
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -664,16 +750,15 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                     float& t = o[i][2 * e + x];
                     if constexpr (PACK) t = whole(t, o[i][2 + x]);
                     t *= 1.0f / kUp;
-                    fin &= fabsf(t) <= 3.402823466e38f;
+                    nan |= t != t;
                 }
-            const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, !fin);
+            if constexpr (!PACK) {
+                const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, nan);
 #pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if ((lanes >> (4 * r)) & 0xFu) bad |= 1u << (r + 8 * e);
+                for (int r = 0; r < 8; ++r)
+                    if ((lanes >> (4 * r)) & 0xFu) bad |= 1u << (r + 8 * e);
+            }
         }
-        // One token sees whatever is read for it: such sums are what they are.  (In 16 rows a weight's two halves meet in one sum, and
-        // their signs may make an infinity NaN: those are taken again.)
-        if (PACK && q.s.n == 1) bad = 0;
         if (tig == 0) {
 #pragma unroll
             for (int e = 0; e < NR; ++e) {
@@ -707,32 +792,8 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                     *reinterpret_cast<float2*>(mine + few_place<DW>(gid + 8 * e, 8 * i + 2 * tig)) = make_float2(t[0], t[1]);
                 }
             __syncwarp();
-            for (uint32_t left = bad; left != 0; left &= left - 1) {  // again, over what the row sees alone
-                const int r = __ffs(left) - 1;
-                const FewRow fr = few_row(f, q, kv_head, group, r);
-                RowState<D> st;
-                float qv[D / 32];
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    st.acc[x] = 0.0f;
-                    qv[x] = fr.live ? f.a.scale * typed_value(f.a.q, f.a.q_type, fr.t * f.a.ldq + static_cast<int64_t>(fr.h) * D + lane * (D / 32) + x) : 0.0f;
-                }
-                for (int k = 0; fr.live && k < n_chunks; ++k) {
-                    const int v0 = ((con.t0 + k) * W + warp) * kFewChunk;
-                    for (int v = v0; v < min(v0 + kFewChunk, q.nv); ++v) {
-                        const int p = few_pos(q, v);
-                        if (few_sees(f.a.mask, fr.pos, p)) attend_row<D, CT>(f.a.w, con.b, kv_head, qv, p, p + 1, st);
-                    }
-                }
-#pragma unroll
-                for (int x = 0; x < D / 32; ++x) {
-                    const int d = lane * (D / 32) + x - part * DW;
-                    if (d >= 0 && d < DW) mine[few_place<DW>(r, d)] = st.acc[x];
-                }
-                if (lane == 0) {
-                    sm_m[warp][r] = st.m;
-                    sm_l[warp][r] = st.l;
-                }
+            if constexpr (!PACK) {
+                if (bad != 0) few_infinite<D, CT, W>(f, con, warp, bad, part, mine);
                 __syncwarp();
             }
             if (ONE && part == 0) cluster_wait();  // the peers are running
