@@ -784,7 +784,8 @@ afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, in
  * own position, or fewer sequences with several new tokens (kv->n_tokens = T; rows behind the last sequence pass through the
  * operators but see nothing: their attention output keeps what AFX_BUF_ATTN held).  The kernels of afx_layer_step with the
  * attention replaced: q | k | v operator, afx_paged_append (the model's rotary table; per-head norms where gains are given, eps as the
- * model's; positions below max_seq), afx_paged_attn on the unrounded fp32 queries, o, gate/up and down operators.  Cross-layer modes
+ * model's; positions below max_seq: a token beyond is left out of the cache and sees nothing, like a row behind the last sequence, AFX_ERR_CAPACITY),
+ * afx_paged_attn on the unrounded fp32 queries, o, gate/up and down operators.  Cross-layer modes
  * as in afx_layer_step.
  *
  *   kv        n_kv_heads and head_dim as the model's; its pages belong to THIS layer; dtype of its own.

@@ -659,7 +659,7 @@ extern "C" afx_status afx_layer_step_paged(afx_model* m, int layer, afx_state* s
     };
     auto attend = [&](const afx_paged_kv& c) {
         return paged_attn(&c, rotated, AFX_F32, ldq, d.n_heads, 0.0f, window, sinks, attn, d.dtype, nullptr, workspace, attn_bytes,
-                          true, dev_status, stream);
+                          d.max_seq, true, dev_status, stream);
     };
     // both calls' checks (without sequences they launch nothing) before anything is enqueued
     afx_paged_kv none = *kv;

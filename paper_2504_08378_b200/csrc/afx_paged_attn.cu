@@ -25,7 +25,7 @@ extern "C" size_t afx_paged_attn_workspace_bytes(const afx_paged_kv* kv, int n_h
 
 afx_status afx::paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads, float scale, int window,
                            int sinks, void* out, int out_dtype, float* lse, void* workspace, size_t workspace_bytes,
-                           bool past_final, int32_t* dev_status, void* stream) {
+                           int limit, bool past_final, int32_t* dev_status, void* stream) {
     PagedAttnArgs a = {};
     const afx_status rc = attn_args(kv, n_heads, dev_status, &a);
     if (rc != AFX_OK) return rc;
@@ -63,6 +63,7 @@ afx_status afx::paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, i
         PagedFewArgs f = {};
         f.a = a;
         f.most = most;
+        f.limit = limit;
         f.past_final = past_final && kv->n_seqs == 1;
         f.joins = static_cast<FewJoin*>(workspace);
         f.slots = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_slots_at());
@@ -76,5 +77,5 @@ extern "C" afx_status afx_paged_attn(const afx_paged_kv* kv, const void* q, int 
                                      float scale, int window, int sinks, void* out, int out_dtype, float* lse,
                                      void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
     return afx::paged_attn(kv, q, q_dtype, ldq, n_heads, scale, window, sinks, out, out_dtype, lse, workspace, workspace_bytes,
-                           false, dev_status, stream);
+                           1 << 30, false, dev_status, stream);
 }

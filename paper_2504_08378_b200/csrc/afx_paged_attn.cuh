@@ -20,9 +20,10 @@ struct PagedAttnArgs {
 };
 
 // afx_paged_attn (afx_paged_attn.cu).  past_final: the kernel in front of it in the stream is the afx_paged_append of the same
-// tokens, and was itself let in by a kernel that waits for all before it.
+// tokens, and was itself let in by a kernel that waits for all before it.  limit: tokens at positions from there on take no part (only
+// where max_new <= AFX_MAX_T).
 afx_status paged_attn(const afx_paged_kv* kv, const void* q, int q_dtype, int64_t ldq, int n_heads, float scale, int window,
-                      int sinks, void* out, int out_dtype, float* lse, void* workspace, size_t workspace_bytes, bool past_final,
+                      int sinks, void* out, int out_dtype, float* lse, void* workspace, size_t workspace_bytes, int limit, bool past_final,
                       int32_t* dev_status, void* stream);
 
 constexpr float kLn2 = 0.6931471805599453f;

@@ -69,6 +69,7 @@ struct PagedFewArgs {
     uint32_t rep_mul;    // r / rep = (r * rep_mul) >> 32 for 0 <= r < 2^16 (rep > 1)
     FewJoin* joins;
     float* slots;
+    int limit;           // tokens at positions from there on take no part
     bool past_final;     // what lies before the new tokens is final since two kernels ago
 };
 
@@ -98,6 +99,7 @@ __device__ __forceinline__ FewSeq few_seq(const PagedFewArgs& f, int b, int row0
     FewSeq q;
     q.s = paged_span(f.a.w, b, row0, report);
     if (q.s.n > f.most) q.s.n = 0;
+    q.s.n = min(q.s.n, max(f.limit - q.s.first, 0));
     const int first = max(q.s.first, 0), end = min(q.s.len, q.s.first + q.s.n);
     q.low = paged_low(f.a.mask, first);
     q.few = paged_few(f.a.mask, q.low);

@@ -287,3 +287,35 @@ def test_sequences_that_share_pages_see_each_others_new_tokens():
     # fp16 rows of values below 8: two roundings of half a step each, and sums of 150 weights in 32 bits
     assert (got - want).abs().max() <= 2 * 2.0 ** -11 * 8
     m.close()
+
+
+@pytest.mark.parametrize("lens,news,out_of", [([40, 66], [1, 1], [1]), ([66], [4], [2, 3]), ([70, 9], [3, 2], [0, 1, 2])])
+def test_tokens_beyond_max_seq_are_left_out(lens, news, out_of):
+    """Their queries do not exist: the attention has nothing to take from what an earlier call left in the workspace."""
+    T, heads, kvh = sum(news), 4, 2
+    m, _ = make("f16", heads, kvh, T, max_seq=64)
+    p = Problem(lens, news, heads, kvh, 128, 16, "f16", seed=3)
+    kvd = p.upload(afx)
+    h0 = torch.randn((T, m.hidden), generator=p.g).cuda()
+    need = afx.afx_layer_paged_workspace_bytes(m.handle, kvd)
+    results = []
+    for fill in (0x00, 0x3C, 0xFF):  # zeros, ordinary numbers, NaN
+        p.d_both.copy_(p.both)
+        ws = torch.full((need + 256,), fill, dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        m.h.copy_(h0)
+        m.bits(afx.BUF_ATTN).fill_(0x1234)
+        afx.afx_layer_step_paged(m.handle, 0, m.state, kvd, 0, 0, None, None, ws.data_ptr() + -ws.data_ptr() % 256, need, dev_status=status)
+        torch.cuda.synchronize()
+        assert status.item() == 3
+        attn = m.bits(afx.BUF_ATTN).cpu()
+        for t in range(T):
+            assert bool((attn[t] == 0x1234).all()) == (t in out_of)
+        results.append((attn, m.h.cpu().clone()))
+    assert all(torch.equal(a, results[0][0]) and torch.equal(h, results[0][1]) for a, h in results)
+    # the cache rows of those tokens are as they were
+    for b, n in enumerate(lens):
+        for c in (0, 1):
+            now = p.rows_of(p.d_both.cpu(), b, c)
+            assert torch.equal(now[64:], p.rows_of(p.both, b, c)[64:])
+    m.close()
