@@ -88,7 +88,13 @@ class DecoderModel:
         off = (-raw.data_ptr()) % 256
         self.blob = raw[off:off + nbytes]
         self.state = afx.afx_state_create(self.handle, T, self.blob, nbytes)
-        self._paged_work = None
+        # the paged steps' workspace (its size goes by the model's alone): there before any stream can use it
+        at = self.blob.data_ptr()
+        kv = afx.PagedKV(dtype=afx.F16, n_kv_heads=n_kv_heads, head_dim=head_dim, page_size=1, n_pages=1, n_seqs=T, n_tokens=T, max_new=1,
+                         page_stride=head_dim, pos_stride=head_dim, head_stride=head_dim, table_stride=1, k_pages=at, v_pages=at,
+                         page_table=at, seq_len=at)
+        self._paged_bytes = afx.afx_layer_paged_workspace_bytes(self.handle, kv)
+        self._paged_work = torch.empty(self._paged_bytes + 256, dtype=torch.uint8, device="cuda")
         torch.cuda.synchronize()
 
     def close(self):
@@ -151,11 +157,9 @@ class DecoderModel:
     def layer_step_paged(self, layer: int, kv: "afx.PagedKV", window: int = 0, sinks: int = 0, g_q=None, g_k=None, stream=None,
                          dev_status=None):
         """kv: this layer's pages.  The model keeps one workspace: its paged steps follow one another on the GPU."""
-        need = afx.afx_layer_paged_workspace_bytes(self.handle, kv)
-        if self._paged_work is None or self._paged_work.numel() < need + 256:
-            self._paged_work = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
         base = self._paged_work.data_ptr()
-        afx.afx_layer_step_paged(self.handle, layer, self.state, kv, window, sinks, g_q, g_k, base + -base % 256, need, stream, dev_status)
+        afx.afx_layer_step_paged(self.handle, layer, self.state, kv, window, sinks, g_q, g_k, base + -base % 256, self._paged_bytes, stream,
+                                 dev_status)
 
     def decode_step_paged(self, kvs, window: int = 0, sinks: int = 0, stream=None, dev_status=None):
         """kvs: one afx.PagedKV per layer."""

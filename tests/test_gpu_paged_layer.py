@@ -319,3 +319,21 @@ def test_tokens_beyond_max_seq_are_left_out(lens, news, out_of):
             now = p.rows_of(p.d_both.cpu(), b, c)
             assert torch.equal(now[64:], p.rows_of(p.both, b, c)[64:])
     m.close()
+
+
+@pytest.mark.parametrize("news", [[1], [1, 1, 1], [5, 3]])
+def test_a_step_takes_no_memory(news):
+    """The first step on a stream of the caller's must not be given memory that another stream may still be using."""
+    m, _ = make("f16", 4, 2, sum(news))
+    p = Problem([40 + i for i in range(len(news))], news, 4, 2, 128, 16, "f16")
+    kvd = p.upload(afx)
+    assert afx.afx_layer_paged_workspace_bytes(m.handle, kvd) == m._paged_bytes
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    with torch.cuda.stream(s):
+        m.layer_step_paged(0, kvd)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+    m.close()
