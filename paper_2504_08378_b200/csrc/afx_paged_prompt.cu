@@ -46,9 +46,10 @@ static afx_status launch_prompt(const PagedAttnArgs& a, int skip, cudaStream_t s
     }
     // Both row tiles to a work, where that many works are more than half of the SMs: they share what is loaded, and one's weights
     // are made while the tensor cores work for the other.  Fewer: a row tile to a work, so that twice as many SMs
-    // take part (100 new tokens of 32 / 8 heads: 12.8 and 11.4 us, 512 of 8 / 1 heads 13.8 and 12.3).  (Works: at most; a sequence's rows are
-    // rounded up.)
-    auto works = [&](int rows) { return (static_cast<int64_t>(a.w.n_tokens) * a.rep / rows + a.w.n_seqs) * a.w.n_kv; };
+    // take part (100 new tokens of 32 / 8 heads: 12.8 and 11.4 us, 512 of 8 / 1 heads 13.8 and 12.3).  (Works: at most; the rows
+    // of a sequence that takes part, of more than `skip` tokens, are rounded up.)
+    const int most_seqs = a.w.n_tokens / (skip + 1), parts = most_seqs < a.w.n_seqs ? most_seqs : a.w.n_seqs;
+    auto works = [&](int rows) { return (static_cast<int64_t>(a.w.n_tokens) * a.rep / rows + parts) * a.w.n_kv; };
     const int sms = sm_count() > 0 ? sm_count() : 148;
     const int rows = 2 * works(kPrTiles * kPrRows) > sms ? kPrTiles * kPrRows : kPrRows;
     if (works(rows) > 0x7FFFFFFF) return AFX_ERR_CAPACITY;

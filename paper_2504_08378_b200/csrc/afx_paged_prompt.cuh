@@ -116,10 +116,16 @@ __device__ __forceinline__ uint32_t pr_weights(float s0, float s1, f32x2 scale, 
     return pack2_bits<CT>(p0, p1);
 }
 
+// What a block's first search leaves for the others: the length of the longest work, the works of a kv head, and per lane which of
+// its sequences have works (from .. to - 1, and perhaps some that have none between them) with the first token row of the first.
+struct PrFound {
+    int longest, total;
+    int from[32], to[32], row0[32];
+};
 // Work `place` of the grid: (rows, kv head), kv heads side by side; the works in classes of falling length (a long one
 // that begins last is what everybody waits for), in a class sequence by sequence.  One warp; what it finds goes to
-// *out, nothing when there are not so many.  longest: -1 on the warp's first call; row0: in shared memory, first token rows of the lanes' first sequences.
-__device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, int& longest, int* row0, PrWork* out) {
+// *out; false when there are not so many.  first_call: of the block's.
+__device__ __forceinline__ bool pr_find(const PagedPromptArgs& args, int place, bool first_call, PrFound* found, PrWork* out) {
     const PagedAttnArgs& a = args.a;
     const int pair = place / a.w.n_kv, lane = lane_id();
     auto take = [&](const SeqSpan& s, int b, int i) {  // work i of sequence b
@@ -144,20 +150,16 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         w.boxed = args.box == 1 || w.few + w.end < w.low ? 0 : (w.few + w.end - w.low) / kPrPos;
         *out = w;
     };
-    const bool first_call = longest < 0, report = first_call && blockIdx.x == 0;
+    const bool report = first_call && blockIdx.x == 0;
     if (a.w.n_seqs == 1) {
-        longest = 0;
-        if (lane == 0) {
-            const SeqSpan s = paged_span(a.w, 0, paged_first_row(a.w, 0), report);
-            const int t = pr_works(args, s);
-            if (pair < t) take(s, 0, t - 1 - pair);
-        }
-        return;
+        const SeqSpan s = paged_span(a.w, 0, paged_first_row(a.w, 0), report && lane == 0);
+        const int t = pr_works(args, s);
+        if (lane == 0 && pair < t) take(s, 0, t - 1 - pair);
+        return pair < t;
     }
-    const int n = a.w.n_seqs, per = (n + 31) / 32, i0 = lane * per, i1 = min(n, i0 + per);
+    // (No loop over the sequences is unrolled: the whole kernel is 4 % faster with less code in it.)
     if (first_call) {
-        // (no loop over the sequences is unrolled: the whole kernel is 4 % faster with less code in it)
-        longest = 0;
+        const int n = a.w.n_seqs, per = (n + 31) / 32, i0 = lane * per, i1 = min(n, i0 + per);
         int top = 0;  // the largest start of the lane's sequences, then of the lanes' in front too
 #pragma unroll 1
         for (int i = i0; i < i1; ++i) top = max(top, paged_first_row(a.w, i));
@@ -167,15 +169,36 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
             if (lane >= o) top = max(top, t);
         }
         top = __shfl_up_sync(0xFFFFFFFFu, top, 1);
-        if (i0 < n) row0[lane] = lane > 0 ? max(top, paged_first_row(a.w, i0)) : paged_first_row(a.w, 0);
+        int at = i0 >= n ? 0 : lane > 0 ? max(top, paged_first_row(a.w, i0)) : paged_first_row(a.w, 0);
+        int longest = 0, total = 0, from = i0, to = i0, row0 = 0;
 #pragma unroll 1
-        for (int i = i0, at = row0[lane]; i < i1; ++i) {
+        for (int i = i0; i < i1; ++i) {
             const SeqSpan s = paged_span(a.w, i, at, report);
+            const int t = pr_works(args, s);
+            if (t > 0) {
+                if (total == 0) {
+                    from = i;
+                    row0 = at;
+                }
+                to = i + 1;
+                longest = max(longest, pr_most(args, s, t));
+            }
+            total += t;
             at = s.next;
-            longest = max(longest, pr_most(args, s, pr_works(args, s)));
         }
+        found->from[lane] = from;
+        found->to[lane] = to;
+        found->row0[lane] = row0;
         longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+        total = __reduce_add_sync(0xFFFFFFFFu, total);
+        if (lane == 0) {
+            found->longest = longest;
+            found->total = total;
+        }
+        __syncwarp();
     }
+    if (pair >= found->total) return false;
+    const int longest = found->longest, i0 = found->from[lane], i1 = found->to[lane], row0 = found->row0[lane];
     int before = 0;  // works of the classes in front
     for (int c = 0; c < kPrClasses; ++c) {
         const int most = (longest >> c) + 1, least = (longest >> (c + 1)) + 1;
@@ -185,9 +208,9 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
         };
         int mine = 0, up;
 #pragma unroll 1
-        for (int i = i0, from = row0[lane]; i < i1; ++i) {
-            const SeqSpan s = paged_span(a.w, i, from, false);
-            from = s.next;
+        for (int i = i0, at = row0; i < i1; ++i) {
+            const SeqSpan s = paged_span(a.w, i, at, false);
+            at = s.next;
             mine += in_class(s, pr_works(args, s), up);
         }
         int incl = mine;
@@ -197,23 +220,24 @@ __device__ __forceinline__ void pr_find(const PagedPromptArgs& args, int place, 
             if (lane >= o) incl += t;
         }
         const int all = __shfl_sync(0xFFFFFFFFu, incl, 31);
-        int at = before + incl - mine;
-        if (pair >= at && pair < at + mine) {
-    #pragma unroll 1
-        for (int i = i0, from = row0[lane]; i < i1; ++i) {
-                const SeqSpan s = paged_span(a.w, i, from, false);
-                from = s.next;
+        int nth = before + incl - mine;
+        if (pair >= nth && pair < nth + mine) {
+#pragma unroll 1
+            for (int i = i0, at = row0; i < i1; ++i) {
+                const SeqSpan s = paged_span(a.w, i, at, false);
+                at = s.next;
                 const int t = pr_works(args, s), k = in_class(s, t, up);
-                if (pair - at < k) {
-                    take(s, i, t - 1 - (up + pair - at));
+                if (pair - nth < k) {
+                    take(s, i, t - 1 - (up + pair - nth));
                     break;
                 }
-                at += k;
+                nth += k;
             }
         }
         before += all;
         if (pair < before) break;
     }
+    return true;
 }
 
 template <int D, int CT>
@@ -230,7 +254,7 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     __shared__ Patience patience;
     __shared__ int steps[kPrLoaders];  // of the ring, that each of the loading warps has made in the end
     __shared__ PrWork work[2];
-    __shared__ int row0[32];
+    __shared__ PrFound found;
     __shared__ __align__(16) uint16_t page_ok[8][8];  // per tile of positions (mod 8) and 16 of them: the cache has them
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char* dyn = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -264,17 +288,6 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
     const uint32_t tmem = tmem_at;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-    // One warp of the loaders finds the block's works: the first by its place in the grid, the others by taking over places
-    // whose blocks have not begun (where that is refused they begin as blocks of their own).
-    int longest = -1;
-    if (warp == 11) {
-        if (lane == 0) work[0].b = -1;
-        __syncwarp();
-        pr_find(args, blockIdx.x, longest, row0, &work[0]);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar.work_full[0]);
-    }
 
     // A warp's next work (in its registers), the same for the whole warp; b < 0: there is none.  it counts the block's works.
     auto next_work = [&](int it, PrWork& w) {
@@ -413,7 +426,25 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             int slot = 0, ok_slot = 0;
             uint32_t turn = 0, q_turn = 0;
             bool q_used = false, ok = true;
-            int asked = 0;  // requests made, 0: none is open
+            uint32_t asks = 0;  // for a place in the grid whose block has not begun
+            bool open = false;  // the last one has no answer yet
+            auto ask = [&]() {
+                if (lane == 0) {
+                    mbar_expect(&bar.answered, 16);
+                    clc_ask(&answer, &bar.answered);
+                }
+                ++asks;
+                open = true;
+                __syncwarp();
+            };
+            auto answered = [&]() {  // the place; -1: none
+                ok = wait(&bar.answered, (asks - 1) & 1);
+                open = !ok;
+                const int place = ok ? clc_place(&answer) : -1;
+                fence_proxy_async();
+                __syncwarp();
+                return place;
+            };
             auto room = [&]() { return turn == 0 || wait(&bar.empty[slot], (turn & 1u) ^ 1u); };
             auto step = [&]() {
                 if (++slot == NB) {
@@ -421,19 +452,16 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     ++turn;
                 }
             };
-            for (int it = 0; ok; ++it) {
-                PrWork w;
-                ok = next_work(it, w);
-                if (!ok || w.b < 0) break;
-                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.rows;
-                if (lw == 2) {  // a place in the grid whose block has not begun, if there is one
-                    asked = it + 1;
-                    if (lane == 0) {
-                        mbar_expect(&bar.answered, 16);
-                        clc_ask(&answer, &bar.answered);
-                    }
-                    __syncwarp();
+            // The third warp finds the block's works: the first by its place in the grid (turn -1, without loads), the others by taking over
+            // places whose blocks have not begun (where that is refused they begin as blocks of their own).
+            for (int it = lw == 2 ? -1 : 0; ok; ++it) {
+                PrWork w = {};
+                if (it >= 0) {
+                    ok = next_work(it, w);
+                    if (!ok || w.b < 0) break;
+                    if (lw == 2) ask();
                 }
+                const int n_tiles = max(w.tiles[0], w.tiles[1]), rows = w.rows;
                 const int end = w.end;
                 int64_t off[3], next[3];
                 auto look_up = [&](int j) {
@@ -484,75 +512,80 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                     if (lane != 0) mbar_arrive(&bar.full[slot]);
                 };
                 if (lw < n_boxed) look_up_box(lw);
-                if (n_boxed == 0) look_up(0);
-                for (int j = 0; j < n_tiles; ++j) {
-                    const bool boxed = j < n_boxed, mine = boxed && j % kPrLoaders == lw;
-                    if (!boxed) {
+                if (n_boxed == 0 && it >= 0) look_up(0);
+                for (int j = it < 0 ? -1 : 0; j < n_tiles; ++j) {
+                    if (j >= 0) {
+                        const bool boxed = j < n_boxed, mine = boxed && j % kPrLoaders == lw;
+                        if (!boxed) {
 #pragma unroll
-                        for (int x = 0; x < 3; ++x) off[x] = next[x];
-                    }
-                    if (j + 1 < n_tiles && j + 1 >= n_boxed) look_up(j + 1);
-                    ok = room();
-                    if (!ok) break;
-                    if (!boxed) {
-#pragma unroll
-                        for (int x = 0; x < 3; ++x) {
-                            const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
-                            if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[ok_slot][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
+                            for (int x = 0; x < 3; ++x) off[x] = next[x];
                         }
-                        fill(a.w.k);
-                    } else if (mine) {
-                        const uint32_t m = __ballot_sync(0xFFFFFFFFu, page >= 0);
-                        if (lane < 8) page_ok[ok_slot][lane] = (m >> (lane * 16 / args.box)) & 1u ? 0xFFFFu : 0u;
-                        fill_boxes(&k_map);
-                    } else {
-                        mbar_arrive(&bar.full[slot]);
-                    }
-                    ok_slot = (ok_slot + 1) & 7;
-                    step();
-                    if (j == 0) {
-                        // the 256 query rows, 32 to a turn of the warp; the work before has made its last scores
-                        if (q_used) {
-                            ok = wait(&bar.q_empty, q_turn);
-                            q_turn ^= 1u;
-                            if (!ok) break;
-                        }
-                        q_used = true;
-                        for (int blk = lw; blk < kPrTiles * kPrRows / 32; blk += kPrLoaders) {
-                            const int rr = w.row_base + blk * 32 + lane, i = rr / a.rep;
-                            const int64_t from = rr < rows ? (w.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D : -1;
+                        if (j + 1 < n_tiles && j + 1 >= n_boxed) look_up(j + 1);
+                        ok = room();
+                        if (!ok) break;
+                        if (!boxed) {
 #pragma unroll
-                            for (int k = 0; k < 32 / RPI; ++k) {
-                                const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
-                                const int64_t o = __shfl_sync(0xFFFFFFFFu, from, row);
-                                put(base + Cfg::kQ + (blk / 4) * Cfg::kTile, (blk % 4) * 32 + row, piece,
-                                    reinterpret_cast<const uint16_t*>(a.q) + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+                            for (int x = 0; x < 3; ++x) {
+                                const uint32_t m = __ballot_sync(0xFFFFFFFFu, off[x] >= 0);
+                                if (lane == 0 && lw + x * kPrLoaders < 8) page_ok[ok_slot][lw + x * kPrLoaders] = static_cast<uint16_t>(m);
                             }
+                            fill(a.w.k);
+                        } else if (mine) {
+                            const uint32_t m = __ballot_sync(0xFFFFFFFFu, page >= 0);
+                            if (lane < 8) page_ok[ok_slot][lane] = (m >> (lane * 16 / args.box)) & 1u ? 0xFFFFu : 0u;
+                            fill_boxes(&k_map);
+                        } else {
+                            mbar_arrive(&bar.full[slot]);
                         }
-                        when_landed(&bar.q_full);
+                        ok_slot = (ok_slot + 1) & 7;
+                        step();
+                        if (j == 0) {
+                            // the 256 query rows, 32 to a turn of the warp; the work before has made its last scores
+                            if (q_used) {
+                                ok = wait(&bar.q_empty, q_turn);
+                                q_turn ^= 1u;
+                                if (!ok) break;
+                            }
+                            q_used = true;
+                            for (int blk = lw; blk < kPrTiles * kPrRows / 32; blk += kPrLoaders) {
+                                const int rr = w.row_base + blk * 32 + lane, i = rr / a.rep;
+                                const int64_t from = rr < rows ? (w.row0 + i) * a.ldq + static_cast<int64_t>(w.kv_head * a.rep + rr - i * a.rep) * D : -1;
+#pragma unroll
+                                for (int k = 0; k < 32 / RPI; ++k) {
+                                    const int row = k * RPI + lane / PIECES, piece = lane % PIECES;
+                                    const int64_t o = __shfl_sync(0xFFFFFFFFu, from, row);
+                                    put(base + Cfg::kQ + (blk / 4) * Cfg::kTile, (blk % 4) * 32 + row, piece,
+                                        reinterpret_cast<const uint16_t*>(a.q) + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
+                                }
+                            }
+                            when_landed(&bar.q_full);
+                        }
+                        ok = room();
+                        if (!ok) break;
+                        if (!boxed) {
+                            fill(a.w.v);
+                        } else if (mine) {
+                            fill_boxes(&v_map);
+                            if (j + kPrLoaders < n_boxed) look_up_box(j + kPrLoaders);
+                        } else {
+                            mbar_arrive(&bar.full[slot]);
+                        }
+                        step();
                     }
-                    ok = room();
-                    if (!ok) break;
-                    if (!boxed) {
-                        fill(a.w.v);
-                    } else if (mine) {
-                        fill_boxes(&v_map);
-                        if (j + kPrLoaders < n_boxed) look_up_box(j + kPrLoaders);
-                    } else {
-                        mbar_arrive(&bar.full[slot]);
-                    }
-                    step();
                     if (lw == 2 && j == min(2, n_tiles - 1)) {
                         // the next work, as soon as this one's first tiles are on their way
-                        ok = wait(&bar.answered, it & 1);
-                        if (ok) asked = 0;
-                        const int place = ok ? clc_place(&answer) : -1;
-                        fence_proxy_async();
+                        int place = it < 0 ? static_cast<int>(blockIdx.x) : answered();
                         if (ok && it >= 1) ok = wait(&bar.work_empty[(it + 1) & 1], (((it + 1) >> 1) & 1) ^ 1);
                         if (!ok) break;
                         if (lane == 0) work[(it + 1) & 1].b = -1;
                         __syncwarp();
-                        if (place >= 0) pr_find(args, place, longest, row0, &work[(it + 1) & 1]);
+                        // places behind the last work (the grid is as large as the call could need) are taken over and left: less than a block each
+                        for (bool first = it < 0; place >= 0 && !pr_find(args, place, first, &found, &work[(it + 1) & 1]); first = false) {
+                            if (lane == 0) *const_cast<volatile uint32_t*>(&patience.told) = nanoseconds();
+                            ask();
+                            place = answered();
+                        }
+                        if (!ok) break;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&bar.work_full[(it + 1) & 1]);
                         __syncwarp();
@@ -560,10 +593,8 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (!ok) {
-                if (lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
-                if (asked > 0) mbar_drain(&bar.answered, (asked - 1) & 1);  // the answer is written before the block ends
-            }
+            if (lane == 0 && !ok) report_status(a.w.status, AFX_ERR_TIMEOUT);
+            if (open) mbar_drain(&bar.answered, (asks - 1) & 1);  // the answer is written before the block ends
             if (lane == 0) steps[lw] = static_cast<int>(turn) * NB + slot;
         }
     } else {
