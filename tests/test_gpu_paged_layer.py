@@ -337,3 +337,34 @@ def test_a_step_takes_no_memory(news):
     torch.cuda.synchronize()
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
     m.close()
+
+
+@pytest.mark.parametrize("depth", [2, 3])
+def test_cross_layer_reuse_over_pages(depth):
+    """Channels predicted by an earlier layer, without synchronisation and step by step: the same bits; and not those of
+    a model without prediction."""
+    T, heads, kvh, n_layers, n_tok = 2, 4, 2, 4, 5
+    runs = []
+    for mode, idle in ((afx.XL_REUSE, True), (afx.XL_REUSE, False), (afx.XL_OFF, True)):
+        m, _ = make("bf16", heads, kvh, T, n_layers, xl_depth=depth, xl_mode=mode) if mode != afx.XL_OFF else make("bf16", heads, kvh, T, n_layers)
+        probs = [Problem([60 + n_tok, 9 + n_tok], [1] * T, heads, kvh, 128, 16, "f16", seed=l) for l in range(n_layers)]
+        kvs = [p.upload(afx) for p in probs]
+        hs = torch.randn((n_tok, T, m.hidden), generator=torch.Generator().manual_seed(5)).cuda()
+        lens = torch.tensor([60, 9], dtype=torch.int32, device="cuda")
+        outs = torch.zeros((n_tok, T, m.hidden), device="cuda")
+        for t in range(n_tok):
+            lens.add_(1)
+            for p in probs:
+                p.d_len.copy_(lens)
+            m.h.copy_(hs[t])
+            for l in range(n_layers):
+                m.layer_step_paged(l, kvs[l])
+                if idle:
+                    torch.cuda.synchronize()
+            outs[t].copy_(m.h)
+        torch.cuda.synchronize()
+        runs.append((outs.clone(), [p.d_both.view(torch.int16).clone() for p in probs]))
+        m.close()
+    assert torch.isfinite(runs[0][0]).all()
+    assert torch.equal(runs[0][0], runs[1][0]) and all(torch.equal(a, b) for a, b in zip(runs[0][1], runs[1][1]))
+    assert not torch.equal(runs[0][0], runs[2][0])

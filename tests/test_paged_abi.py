@@ -116,3 +116,11 @@ def test_descriptors_have_the_headers_layout(tmp_path):
         body = re.search(r"typedef struct \{([^}]*)\}\s*" + c + r"\s*;", hdr).group(1)
         names = [re.search(r"(\w+)\s*$", part).group(1) for decl in body.split(";") if decl.strip() for part in decl.split(",")]
         assert names == [n for n, _ in cls._fields_]
+
+
+def test_counts_of_query_heads_are_checked_one_by_one():
+    assert attn(heads=12) == 1
+    assert attn(heads=0) == 1
+    assert attn(heads=-8) == 1
+    assert attn(heads=16000, ldq=16000 * 128) == 3
+    assert attn(desc(n_seqs=1, n_tokens=1 << 23, max_new=1 << 23, tok_start=FAKE), heads=512, ldq=512 * 128) == 3  # rows times heads
