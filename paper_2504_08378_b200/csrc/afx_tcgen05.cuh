@@ -64,9 +64,10 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     const uint32_t t0 = nanoseconds();
 #pragma unroll 1
     while (!mbar_try_wait(bar, parity)) {
-        const uint32_t told = shared->told, t = nanoseconds();  // (in this order: no age is negative)
+        // (a word that is written while it is read may be younger than the clock's reading: a millisecond more, so that no age is negative)
+        const uint32_t told = shared->told, t = nanoseconds();
         if (shared->gave_up != 0) return false;
-        if (min(t - t0, t - told) > static_cast<uint32_t>(AFX_WAIT_NS)) {
+        if (min(t - t0, t - told + (1u << 20)) > static_cast<uint32_t>(AFX_WAIT_NS)) {
             shared->gave_up = 1;
             return false;
         }
