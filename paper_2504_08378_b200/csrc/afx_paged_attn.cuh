@@ -34,15 +34,6 @@ __device__ __forceinline__ float2 pair_values(uint32_t r) {
     return make_float2(__uint_as_float(r << 16), __uint_as_float(r & 0xFFFF0000u));
 }
 
-__device__ __forceinline__ float typed_value(const char* p, int type, int64_t i) {
-    if (type == AFX_F32) return reinterpret_cast<const float*>(p)[i];
-    const uint16_t b = reinterpret_cast<const uint16_t*>(p)[i];
-    return type == AFX_F16 ? bits_to_float<AFX_F16>(b) : bits_to_float<AFX_BF16>(b);
-}
-__device__ __forceinline__ uint16_t typed_bits(float v, int type) {
-    return type == AFX_F16 ? float_to_bits<AFX_F16>(v) : float_to_bits<AFX_BF16>(v);
-}
-
 // The sign's places of the halves that are infinite or NaN.  (An exponent of ones carries there.)
 template <int CT>
 __device__ __forceinline__ uint32_t not_finite(uint32_t pair) {
@@ -53,61 +44,23 @@ __device__ __forceinline__ uint32_t not_finite(const uint4& x) {
     return not_finite<CT>(x.x) | not_finite<CT>(x.y) | not_finite<CT>(x.z) | not_finite<CT>(x.w);
 }
 
-// Running softmax of one row in a warp: a lane owns D / 32 neighbouring dims.
-template <int D>
-struct RowState {
-    float m = -INFINITY, l = 0.0f, acc[D / 32];
-};
-
-// Positions [from, to) of (sequence b, kv head g) added to the row with query q (times scale * log2 e), four on their way at
-// once.  Nothing more is added once every sum is infinite or NaN: none becomes finite again.
-template <int D, int CT>
-__device__ __forceinline__ void attend_row(const PagedView& w, int b, int g, const float (&q)[D / 32], int from, int to,
-                                           RowState<D>& s) {
-    constexpr int E = D / 32, U = 4;
-    const int lane = lane_id();
-    for (int p0 = from; p0 < to; p0 += U) {
-        uint32_t kr[U][E / 2], vr[U][E / 2];
-        bool in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = p0 + u < to ? paged_row(w, b, p0 + u, g) : -1;
-            in[u] = at >= 0;
-            if (at < 0 && p0 + u < to && lane == 0) report_status(w.status, AFX_ERR_INVALID_ARG);
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                kr[u][i] = in[u] ? reinterpret_cast<const uint32_t*>(w.k + at)[lane * (E / 2) + i] : 0u;
-                vr[u][i] = in[u] ? reinterpret_cast<const uint32_t*>(w.v + at)[lane * (E / 2) + i] : 0u;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!in[u]) continue;
-            float d = 0.0f, v[E];
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-                const float2 kk = pair_values<CT>(kr[u][i]), vv = pair_values<CT>(vr[u][i]);
-                d = fmaf(q[2 * i], kk.x, d);
-                d = fmaf(q[2 * i + 1], kk.y, d);
-                v[2 * i] = vv.x;
-                v[2 * i + 1] = vv.y;
-            }
-            d = warp_sum(d);
-            const float mn = fmaxf(s.m, d);
-            const float ref = mn == -INFINITY ? 0.0f : mn;
-            const float f = fast_exp2(s.m - ref), pw = fast_exp2(d - ref);
-            s.m = mn;
-            s.l = fmaf(s.l, f, pw);
-#pragma unroll
-            for (int i = 0; i < E; ++i) s.acc[i] = fmaf(s.acc[i], f, pw * v[i]);
-        }
-        if (to - from > U) {
-            bool some = false;
-#pragma unroll
-            for (int i = 0; i < E; ++i) some |= fabsf(s.acc[i]) <= 3.402823466e38f;
-            if (!__any_sync(0xFFFFFFFFu, some)) return;
-        }
-    }
+// C += A B of 16 x 16 and 16 x 8 values, fp32 sums.
+template <int CT>
+__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (CT == AFX_F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of which a lane holds two neighbours of a row, the other way round.
+__device__ __forceinline__ uint32_t transposed_8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 
 // Whether one of the values at positions [from, to) of (sequence b, kv head g) is infinite or NaN; the same for the warp.

@@ -262,17 +262,6 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t at)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
                  : "r"(at));
 }
-template <int CT>
-__device__ __forceinline__ void few_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if constexpr (CT == AFX_F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 // (a, b) rounded to the cache's type, and what that left out
 template <int CT>
 __device__ __forceinline__ void few_split(float a, float b, uint32_t& hi, uint32_t& lo) {
@@ -613,11 +602,11 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                 for (int j = 0; j < NK; ++j) {
                     uint32_t kb[4];
                     ldmatrix_x4(kb, kat + row * (D * 2) + (((2 * j + half) ^ (row & 7)) << 4));
-                    few_mma<CT>(c[0], qa[j], kb[0], kb[1]);
-                    few_mma<CT>(c[1], qa[j], kb[2], kb[3]);
+                    mma_16816<CT>(c[0], qa[j], kb[0], kb[1]);
+                    mma_16816<CT>(c[1], qa[j], kb[2], kb[3]);
                     if constexpr (QF32 && !PACK) {
-                        few_mma<CT>(cl[0], ql[j], kb[0], kb[1]);
-                        few_mma<CT>(cl[1], ql[j], kb[2], kb[3]);
+                        mma_16816<CT>(cl[0], ql[j], kb[0], kb[1]);
+                        mma_16816<CT>(cl[1], ql[j], kb[2], kb[3]);
                     }
                 }
             }
@@ -724,11 +713,11 @@ __global__ void __launch_bounds__(ONE ? kOneWarps * 32 : kFewThreads, ONE ? 1 : 
                 for (int i = 0; i < NT; i += 2) {
                     uint32_t vb[4];
                     ldmatrix_x4_trans(vb, vat + row * (D * 2) + (((i + half) ^ (row & 7)) << 4));
-                    few_mma<CT>(o[i], pa, vb[0], vb[1]);
-                    few_mma<CT>(o[i + 1], pa, vb[2], vb[3]);
+                    mma_16816<CT>(o[i], pa, vb[0], vb[1]);
+                    mma_16816<CT>(o[i + 1], pa, vb[2], vb[3]);
                     if constexpr (!PACK) {
-                        few_mma<CT>(o[i], pl, vb[0], vb[1]);
-                        few_mma<CT>(o[i + 1], pl, vb[2], vb[3]);
+                        mma_16816<CT>(o[i], pl, vb[0], vb[1]);
+                        mma_16816<CT>(o[i + 1], pl, vb[2], vb[3]);
                     }
                 }
             }

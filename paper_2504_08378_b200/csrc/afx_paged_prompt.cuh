@@ -240,6 +240,150 @@ __device__ __forceinline__ bool pr_find(const PagedPromptArgs& args, int place, 
     return true;
 }
 
+// Rows 16 half .. + 15 of a warp, those of `left` among them, over what each sees alone: its lanes hold the rows' tokens, heads and
+// positions.  Sixteen positions at a time, products of 16 x 8 x 16 straight from the cache; values that are not finite are added to the rows that see
+// them and are zeros for the product.  (A warp's 32 rows over 40000 positions, D = 64: 8 ms; a row at a time they took 500.)  That may take long, and the
+// block's other warps wait for it with the next work: they are told that it goes on.
+template <int D, int CT>
+__device__ __forceinline__ void pr_again(const PagedAttnArgs& a, const PrWork& w, int half, uint32_t left, int token, int head, int pos,
+                                         Patience* patience) {
+    constexpr int NK = D / 16, NT = D / 8;
+    constexpr float kUpLog = CT == AFX_F16 ? 7.0f : 0.0f;
+    const int lane = lane_id(), gid = lane >> 2, tig = lane & 3;
+    uint32_t q[NK][4];
+    float o[NT][4], m[2], l[2];
+    int64_t at[2];  // the rows' places in out
+    int p_row[2];
+    bool mine[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int r = 16 * half + gid + 8 * e;
+        const int t = w.row0 + __shfl_sync(0xFFFFFFFFu, token, r), hd = __shfl_sync(0xFFFFFFFFu, head, r);
+        const int p = __shfl_sync(0xFFFFFFFFu, pos, r);
+        mine[e] = (left >> r) & 1u;
+        p_row[e] = mine[e] ? p : -1;
+        at[e] = (static_cast<int64_t>(t) * a.heads + hd) * D;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint16_t*>(a.q) + t * a.ldq + static_cast<int64_t>(hd) * D);
+#pragma unroll
+        for (int i = 0; i < 2 * NK; ++i) q[i >> 1][2 * (i & 1) + e] = mine[e] ? src[4 * i + tig] : 0u;
+        m[e] = -INFINITY;
+        l[e] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[i][x] = 0.0f;
+    const int last = __reduce_max_sync(0xFFFFFFFFu, max(p_row[0], p_row[1]));
+    const int first = __reduce_min_sync(0xFFFFFFFFu, min(p_row[0] < 0 ? last : p_row[0], p_row[1] < 0 ? last : p_row[1]));
+    const int low = paged_low(a.mask, max(first, 0)), few = paged_few(a.mask, low), nv = last < 0 ? 0 : few + last + 1 - low;
+#pragma unroll 1
+    for (int v0 = 0; v0 < nv; v0 += 16) {
+        if (v0 % AFX_TELL_EVERY == 0 && lane == 0) *const_cast<volatile uint32_t*>(&patience->told) = nanoseconds();
+        if (v0 % 64 == 0) {  // once every sum is infinite or NaN nothing more is added: none becomes finite again
+            bool some = false;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) some |= mine[e] && (fabsf(o[i][2 * e]) <= 3.402823466e38f || fabsf(o[i][2 * e + 1]) <= 3.402823466e38f);
+            if (!__any_sync(0xFFFFFFFFu, some)) break;
+        }
+        const int v = v0 + (lane & 15);
+        const int64_t row = v < nv ? paged_row(a.w, w.b, v < few ? v : v - few + low, w.kv_head) : -1;
+        const uint32_t there = __ballot_sync(0xFFFFFFFFu, row >= 0);
+        uint32_t raw[2][NT];  // values of position 8 t + gid
+        float c[2][4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t from = __shfl_sync(0xFFFFFFFFu, row, 8 * t + gid);
+            const uint32_t* k = reinterpret_cast<const uint32_t*>(a.w.k + (from < 0 ? 0 : from)) + tig;
+            const uint32_t* vv = reinterpret_cast<const uint32_t*>(a.w.v + (from < 0 ? 0 : from)) + tig;
+            uint32_t kb[2 * NK];
+#pragma unroll
+            for (int i = 0; i < 2 * NK; ++i) kb[i] = from < 0 ? 0u : k[4 * i];
+#pragma unroll
+            for (int i = 0; i < NT; ++i) raw[t][i] = from < 0 ? 0u : vv[4 * i];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) c[t][x] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NK; ++j) mma_16816<CT>(c[t], q[j], kb[2 * j], kb[2 * j + 1]);
+        }
+        uint32_t pa[4];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float s[4], top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int j = 8 * (x >> 1) + 2 * tig + (x & 1), vj = v0 + j, p = vj < few ? vj : vj - few + low;
+                const bool sees = ((there >> j) & 1u) && p <= p_row[e] && (a.mask.window == 0 || p > p_row[e] - a.mask.window || p < a.mask.sinks);
+                s[x] = sees ? c[x >> 1][2 * e + (x & 1)] * a.scale : -INFINITY;
+                top = fmaxf(top, s[x]);
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = fmaxf(fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2)), m[e]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            const float f = fast_exp2(m[e] - ref);  // 0 where nothing was seen before
+            m[e] = top;
+            l[e] *= f;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                o[i][2 * e] *= f;
+                o[i][2 * e + 1] *= f;
+            }
+            float wt[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                wt[x] = fast_exp2(s[x] - ref + kUpLog);
+                l[e] += wt[x];
+            }
+            pa[e] = pack2_bits<CT>(wt[0], wt[1]);
+            pa[2 + e] = pack2_bits<CT>(wt[2], wt[3]);
+        }
+        uint32_t found = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < NT; ++i) found |= not_finite<CT>(raw[t][i]);
+        if (__any_sync(0xFFFFFFFFu, found != 0u)) {
+#pragma unroll 1
+            for (int j = 0; j < 16; ++j) {
+                const int vj = v0 + j, p = vj < few ? vj : vj - few + low;
+                bool sees[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    sees[e] = ((there >> j) & 1u) && p <= p_row[e] && (a.mask.window == 0 || p > p_row[e] - a.mask.window || p < a.mask.sinks);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const float2 x = pair_values<CT>(__shfl_sync(0xFFFFFFFFu, j < 8 ? raw[0][i] : raw[1][i], 4 * (j & 7) + tig));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (sees[e] && !(fabsf(x.x) <= 3.402823466e38f)) o[i][2 * e] += x.x;
+                        if (sees[e] && !(fabsf(x.y) <= 3.402823466e38f)) o[i][2 * e + 1] += x.y;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < NT; ++i) raw[t][i] &= ~((not_finite<CT>(raw[t][i]) >> 15) * 0xFFFFu);
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) mma_16816<CT>(o[i], pa, transposed_8x8(raw[0][i]), transposed_8x8(raw[1][i]));
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 1);
+        l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 2);
+        if (!mine[e]) continue;
+        const float inv = l[e] == 0.0f ? 0.0f : 1.0f / l[e];
+        uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + at[e]) + tig;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const float x = l[e] == 0.0f ? 0.0f : o[i][2 * e] * inv, y = l[e] == 0.0f ? 0.0f : o[i][2 * e + 1] * inv;
+            dst[4 * i] = a.out_type == AFX_F16 ? pack2_bits<AFX_F16>(x, y) : pack2_bits<AFX_BF16>(x, y);
+        }
+    }
+}
+
 template <int D, int CT>
 __global__ void __launch_bounds__(kPrThreads, 1)
 paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
@@ -746,16 +890,17 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
             }
             // Rows whose sums are not finite.  Where they see what is not finite, that is what they are; but a weight of zero times a NaN or
             // an infinity that a row does not see has to be nothing.  Only the tiles at the ends of what the rows see hold places that
-            // are masked: if a value there is not finite, the rows are taken again, over what they see alone, on the fp32 pipe.
+            // are masked: if a value there is not finite, the rows are taken again, over what they see alone.
             bool again = false;
             if (__any_sync(0xFFFFFFFFu, live && !fin)) {
                 const uint32_t there = __ballot_sync(0xFFFFFFFFu, live);  // (the warp's rows in front)
                 const int lo = max(__shfl_sync(0xFFFFFFFFu, pos, 0), -1), hi = __shfl_sync(0xFFFFFFFFu, pos, there != 0 ? 31 - __clz(there) : 0);
                 const int back = min(w.end, w.tiles[x] * kPrPos - shift);  // behind the last tile's places
-                again = any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, max(lo + 1, 0), back);
-                if (a.mask.window > 0) {
-                    again |= any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, w.low, min(max(hi - a.mask.window + 1, w.low), w.end));
-                    again |= any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, min(a.mask.sinks, w.few), w.few);
+#pragma unroll 1
+                for (int part = 0; part < (a.mask.window > 0 ? 3 : 1) && !again; ++part) {
+                    const int from = part == 0 ? max(lo + 1, 0) : part == 1 ? w.low : min(a.mask.sinks, w.few);
+                    const int to = part == 0 ? back : part == 1 ? min(max(hi - a.mask.window + 1, w.low), w.end) : w.few;
+                    again = any_value_not_finite<D, CT>(a.w, w.b, w.kv_head, from, to);
                 }
             }
             if (live && (fin || !again)) {
@@ -781,34 +926,13 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                 }
             }
             if (live && a.lse != nullptr) a.lse[at] = none ? -INFINITY : (m + log2f(l) - kUpLog) * kLn2;  // (the values have no part in it)
-            uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin && again);
-            for (; left != 0; left &= left - 1) {
-                const int who = __ffs(left) - 1;
-                const int wi = __shfl_sync(0xFFFFFFFFu, i, who), wh = __shfl_sync(0xFFFFFFFFu, h, who);
-                const int wp = __shfl_sync(0xFFFFFFFFu, pos, who);
-                constexpr int E = D / 32;
-                RowState<D> st;
-                float q[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    st.acc[e] = 0.0f;
-                    q[e] = a.scale * typed_value(a.q, a.q_type, (w.row0 + wi) * a.ldq + static_cast<int64_t>(wh) * D + lane * E + e);
+            const uint32_t left = __ballot_sync(0xFFFFFFFFu, live && !fin && again);
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half)
+                if (((left >> (16 * half)) & 0xFFFFu) != 0u) {
+                    const int rr2 = w.row_base + x * kPrRows + (warp & 3) * 32 + lane, i2 = rr2 / a.rep;
+                    pr_again<D, CT>(a, w, half, left, i2, w.kv_head * a.rep + rr2 - i2 * a.rep, rr2 < w.rows ? w.first + i2 : -1, &patience);
                 }
-                // (This may take long, and the block's other warps wait for it with the next work: they are told that it goes on.)
-                const int low = paged_low(a.mask, wp), few = paged_few(a.mask, low);
-                for (int part = 0; wp >= 0 && part < 2; ++part) {
-                    const int end = part == 0 ? few : wp + 1;
-                    for (int from = part == 0 ? 0 : low, to; from < end; from = to) {
-                        to = end - from > AFX_TELL_EVERY ? from + AFX_TELL_EVERY : end;
-                        attend_row<D, CT>(a.w, w.b, w.kv_head, q, from, to, st);
-                        if (lane == 0) *const_cast<volatile uint32_t*>(&patience.told) = nanoseconds();
-                    }
-                }
-                const int64_t wat = static_cast<int64_t>(w.row0 + wi) * a.heads + wh;
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    a.out[wat * D + lane * E + e] = typed_bits(st.l == 0.0f ? 0.0f : st.acc[e] / st.l, a.out_type);
-            }
         }
         if (!ok && lane == 0) report_status(a.w.status, AFX_ERR_TIMEOUT);
     }
