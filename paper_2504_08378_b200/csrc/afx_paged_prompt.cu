@@ -53,6 +53,7 @@ static afx_status launch_prompt(const PagedAttnArgs& a, int skip, cudaStream_t s
     const int sms = sm_count() > 0 ? sm_count() : 148;
     const int rows = 2 * works(kPrTiles * kPrRows) > sms ? kPrTiles * kPrRows : kPrRows;
     if (works(rows) > 0x7FFFFFFF) return AFX_ERR_CAPACITY;
+    if (works(rows) == 0) return AFX_OK;  // (fewer tokens than a sequence that takes part has)
     PagedPromptArgs args = {a, 1, skip, rows};
     CUtensorMap maps[2] = {};
     // (with a window the positions begin on a box's border, and the first ones end on one: small boxes leave less to mask)

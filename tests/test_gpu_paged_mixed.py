@@ -30,3 +30,10 @@ def test_a_chunk_beside_decoding_sequences_costs_what_it_costs_alone(n, chunk):
         times.append(median_us(p, q, 32, 64, p.upload(afx)))
     print([round(t) for t in times])
     assert times[0] <= 2 * (times[1] + times[2])
+
+
+@pytest.mark.parametrize("lens,news", [([50, 60], [4, 4]), ([9, 3, 70], [1, 1, 1]), ([40, 41], [0, 2])])
+def test_a_batch_with_fewer_tokens_than_a_prompt_has(lens, news):
+    """max_new is an upper bound: a batch of a few tokens in all may come with that of a whole prompt."""
+    check(Problem(lens, news, 8, 2, 64, 16, "bf16"), max_new=4096)
+    check(Problem(lens, news, 1, 1, 64, 16, "bf16"), max_new=4096)
