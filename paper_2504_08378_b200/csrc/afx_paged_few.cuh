@@ -7,13 +7,13 @@
 // positions of a tile 16 to a warp (a chunk), every warp with a ring of chunks of its own that cp.async fills across the borders of
 // items: nobody waits for another warp before an item's end.  A chunk is two matrix products on the tensor cores
 // (16 rows x 16 positions x D and 16 rows x D x 16 positions); softmax is online and in base 2, the weights are split
-// into two 16-bit halves so that none of their bits are lost, fp32 queries likewise.  Where there are at most 8 rows (one new token
+// into two 16-bit halves, fp32 queries likewise, which keep 22 of their bits in fp16 and 16 in bf16.  Where there are at most 8 rows (one new token
 // and up to 8 heads per kv head), the two halves are the 16 rows of a product.
 //
 // Bound by HBM: 16 positions are 8 KB of K and V at D = 128 and about 250 instructions of a warp, an SM's share of the
 // bandwidth is 8 KB every 190 ns = 1400 issue slots.  Two blocks of 4 warps per SM with rings of 96 KB each keep
-// up to 128 KB of an SM on their way.  64 windows of 4096 positions, 32 / 8 heads: 160 us, 96 % of the copy rate; 61 sequences of 1 to
-// 8192 positions, 64 / 8 heads: 63 us, 83 %; what is missing is latency (list 1.8 us, first look-ups and rows 2.5, join 3).
+// up to 128 KB of an SM on their way.  64 windows of 4096 positions, 32 / 8 heads: 167 us, 93 % of the copy rate; 61 sequences of 1 to
+// 8192 positions, 64 / 8 heads: 65 us, 81 %; what is missing is latency (list 1.8 us, first look-ups and rows 2.5, join 3).
 #pragma once
 
 #include "afx_attn_mma.cuh"

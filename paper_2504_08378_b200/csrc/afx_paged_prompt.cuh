@@ -19,7 +19,7 @@
 // ends (what lies behind it in its page may be anything, and has to become zero), row by row with cp.async.  (Everything with
 // cp.async: the tensor cores waited 1300 of 4000 cycles per step for the copies.)
 //
-// A step of both row tiles takes 3600 cycles at D = 128 (8192 new tokens of 64 / 8 heads: 1.08 ms, 1020 TFLOP/s, 73 % of cuBLAS in a
+// A step of both row tiles takes 3600 cycles at D = 128 (8192 new tokens of 64 / 8 heads: 1.07 ms, 1030 TFLOP/s, 74 % of cuBLAS in a
 // loop under the power limit), where its 2 x 128 x 128 exponentials are 2048 cycles of the special-function units and
 // its products 2048 cycles of the tensor cores: a row tile's chain (scores, weights, products) is what is long, and the
 // two chains fill each other's gaps only in part.  Exponentials by polynomials on the fp32 pipe for an eighth or a quarter of
