@@ -633,7 +633,9 @@ paged_prompt_kernel(const PagedPromptArgs args, const __grid_constant__ CUtensor
                             put(tile, blk * 16 + row, piece, pages + (o < 0 ? 0 : o) + piece * 8, o < 0 ? 0 : 16);
                         }
                     }
-                    when_landed(&bar.full[slot]);
+                    // (the copies' arrival, and the thread's own, which hands on what it has stored beside them)
+                    asm volatile("cp.async.mbarrier.arrive.shared::cta.b64 [%0];" ::"r"(smem_u32(&bar.full[slot])) : "memory");
+                    mbar_arrive(&bar.full[slot]);
                 };
                 // Tiles that are read in boxes: warp j % 3 reads tile j, a box per lane (and half of the dims).
                 const int n_boxed = w.boxed;
